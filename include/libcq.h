@@ -502,6 +502,86 @@ CQ_API cq_status cq_chunk_attention_rope_paged(const void *q, const void *k_pool
                                         void *out, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Caches that stay bounded.  A sequence that goes on and on either looks at its cache through a window (the first two
+ * groups of calls below), or keeps the tokens that attention weighs most and drops the others (the last two).
+ *
+ * cq_decode_attention_window[_paged] -- cq_decode_attention[_paged] through a sliding window with sinks: the query, at
+ * position p = t - 1 (seq_lens[n] - 1), attends to the tokens i <= p with i > p - window or i < n_sink.
+ *   window            >= 1 (the query's own token is always seen); n_sink >= 0.  Values beyond t mean t
+ *   tokens_per_split  0 = cq_decode_window_default_split(...); otherwise a multiple of 64, of the tokens that are walked:
+ *                     the sinks' 64-token tiles in front of the window, then the window's
+ *   workspace         device, cq_decode_window_workspace_bytes(...) bytes
+ *   everything else as in cq_decode_attention.
+ * Only tiles that hold a token that is seen are read: the time is that of a context of window + n_sink tokens, and in a
+ * paged cache the block table's entries and the pages of all other tiles are not looked at (pages that have left the
+ * window can go to another sequence).  Keys are used as stored; where they were rotated, the positions are the tokens' own.
+ *
+ * cq_decode_step_window[_paged] -- cq_decode_step[_paged] likewise: the new token is encoded at position p and attended to.
+ * Codes and output are bit-identical to cq_encode_kv followed by cq_decode_attention_window.
+ * Errors: as cq_decode_attention and cq_decode_step; CQ_ERR_INVALID_ARG also for window <= 0 or n_sink < 0.
+ */
+CQ_API int32_t cq_decode_window_default_split(const cq_format *fmt, int32_t batch, int32_t n_q_heads, int32_t t, int32_t window, int32_t n_sink);
+CQ_API size_t cq_decode_window_workspace_bytes(const cq_format *fmt, int32_t batch, int32_t n_q_heads, int32_t t, int32_t window, int32_t n_sink,
+                                        int32_t tokens_per_split);
+CQ_API cq_status cq_decode_attention_window(const void *q, const void *k_codes, const void *v_codes,
+                                     const void *k_centroids, const void *v_centroids,
+                                     float scale, const cq_format *fmt,
+                                     int32_t batch, int32_t n_q_heads, int32_t t, int32_t t_cap,
+                                     const int32_t *seq_lens, int32_t window, int32_t n_sink, int32_t tokens_per_split,
+                                     void *out, void *workspace, size_t workspace_bytes, void *stream);
+CQ_API cq_status cq_decode_attention_window_paged(const void *q, const void *k_pool, const void *v_pool,
+                                           const void *k_centroids, const void *v_centroids,
+                                           float scale, const cq_format *fmt,
+                                           int32_t batch, int32_t n_q_heads, int32_t t, const cq_page_table *pages,
+                                           const int32_t *seq_lens, int32_t window, int32_t n_sink, int32_t tokens_per_split,
+                                           void *out, void *workspace, size_t workspace_bytes, void *stream);
+CQ_API cq_status cq_decode_step_window(const void *q, const void *x_k_new, const void *x_v_new, int64_t x_row_stride,
+                                void *k_codes, void *v_codes,
+                                const void *k_centroids, const void *v_centroids,
+                                float scale, const cq_format *fmt,
+                                int32_t batch, int32_t n_q_heads, int32_t t, int32_t t_cap,
+                                const int32_t *seq_lens, int32_t window, int32_t n_sink, int32_t tokens_per_split,
+                                void *out, void *workspace, size_t workspace_bytes, void *stream);
+CQ_API cq_status cq_decode_step_window_paged(const void *q, const void *x_k_new, const void *x_v_new, int64_t x_row_stride,
+                                      void *k_pool, void *v_pool,
+                                      const void *k_centroids, const void *v_centroids,
+                                      float scale, const cq_format *fmt,
+                                      int32_t batch, int32_t n_q_heads, int32_t t, const cq_page_table *pages,
+                                      const int32_t *seq_lens, int32_t window, int32_t n_sink, int32_t tokens_per_split,
+                                      void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * cq_decode_attention_weights[_paged] -- cq_decode_attention[_paged] that also adds up the attention weights: for every
+ * sequence n, KV head h and token i < t (seq_lens[n]),
+ *     weights[n][h][i] = decay * weights[n][h][i] + sum over the query heads of h of softmax(scale q.k)_i
+ * decay 1 sums over all steps, 0 keeps the last step's weights (the accumulators are then written without being read).
+ *   weights           device, fp32 [batch][n_kv_heads][weights_stride], weights_stride >= t floats; positions of a
+ *                     sequence behind its length are left as they are.  A token's accumulator belongs to the caller: zero
+ *                     it when the token is appended
+ *   workspace         device, cq_decode_weights_workspace_bytes(...) bytes (partials, and the scores in fp32)
+ *   everything else as in cq_decode_attention, and the output as there.
+ * Weights are fp32, from fp32 scores; each accumulator is formed by one thread in a fixed order (no atomics), so equal
+ * calls give equal bits.  Two launches.
+ * Errors: as cq_decode_attention; CQ_ERR_INVALID_ARG also for weights null or misaligned, weights_stride < t or a decay
+ * that is not finite.
+ */
+CQ_API size_t cq_decode_weights_workspace_bytes(const cq_format *fmt, int32_t batch, int32_t n_q_heads, int32_t t, int32_t tokens_per_split);
+CQ_API cq_status cq_decode_attention_weights(const void *q, const void *k_codes, const void *v_codes,
+                                      const void *k_centroids, const void *v_centroids,
+                                      float scale, const cq_format *fmt,
+                                      int32_t batch, int32_t n_q_heads, int32_t t, int32_t t_cap,
+                                      const int32_t *seq_lens, int32_t tokens_per_split,
+                                      float *weights, int64_t weights_stride, float decay,
+                                      void *out, void *workspace, size_t workspace_bytes, void *stream);
+CQ_API cq_status cq_decode_attention_weights_paged(const void *q, const void *k_pool, const void *v_pool,
+                                            const void *k_centroids, const void *v_centroids,
+                                            float scale, const cq_format *fmt,
+                                            int32_t batch, int32_t n_q_heads, int32_t t, const cq_page_table *pages,
+                                            const int32_t *seq_lens, int32_t tokens_per_split,
+                                            float *weights, int64_t weights_stride, float decay,
+                                            void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * cq_dequantize -- the inverse lookup ("dequantization", Section 2.2; CQ(A) of Eq. 5 as values):
  * out[n][t][g c + i] = centroids[g][code(n, t_offset + t, g)][i] for t = 0 .. t_count - 1, bit
  * for bit the stored fp16 centroids.  For callers that need dense keys / values (e.g. a

@@ -34,6 +34,9 @@ EXPORTS = (
     "cq_rope_table_bytes", "cq_rope_table", "cq_decode_rope_default_split", "cq_decode_attention_rope",
     "cq_decode_attention_rope_paged", "cq_decode_step_rope", "cq_decode_step_rope_paged",
     "cq_chunk_rope_workspace_bytes", "cq_chunk_attention_rope", "cq_chunk_attention_rope_paged",
+    "cq_decode_window_default_split", "cq_decode_window_workspace_bytes", "cq_decode_attention_window",
+    "cq_decode_attention_window_paged", "cq_decode_step_window", "cq_decode_step_window_paged",
+    "cq_decode_weights_workspace_bytes", "cq_decode_attention_weights", "cq_decode_attention_weights_paged",
     "cq_probe_stream_read", "cq_probe_copy", "cq_probe_mfma", "cq_probe_decode_plan",
 )
 
@@ -189,6 +192,22 @@ def load() -> ctypes.CDLL:
     lib.cq_decode_step_rope_paged.restype = ctypes.c_int
     lib.cq_decode_step_rope_paged.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, ctypes.c_float, fp, i32, i32, i32, pp, vp,
                                               i32, vp, i32, vp, vp, ctypes.c_size_t, vp]
+    f32, size = ctypes.c_float, ctypes.c_size_t
+    lib.cq_decode_window_default_split.restype = i32
+    lib.cq_decode_window_default_split.argtypes = [fp, i32, i32, i32, i32, i32]
+    lib.cq_decode_window_workspace_bytes.restype = size
+    lib.cq_decode_window_workspace_bytes.argtypes = [fp, i32, i32, i32, i32, i32, i32]
+    for at, name in ((i32, "cq_decode_attention_window"), (pp, "cq_decode_attention_window_paged")):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = [vp, vp, vp, vp, vp, f32, fp, i32, i32, i32, at, vp, i32, i32, i32, vp, vp, size, vp]
+    for at, name in ((i32, "cq_decode_step_window"), (pp, "cq_decode_step_window_paged")):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, f32, fp, i32, i32, i32, at, vp, i32, i32, i32, vp, vp, size, vp]
+    lib.cq_decode_weights_workspace_bytes.restype = size
+    lib.cq_decode_weights_workspace_bytes.argtypes = [fp, i32, i32, i32, i32]
+    for at, name in ((i32, "cq_decode_attention_weights"), (pp, "cq_decode_attention_weights_paged")):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = [vp, vp, vp, vp, vp, f32, fp, i32, i32, i32, at, vp, i32, vp, i64, f32, vp, vp, size, vp]
     lib.cq_probe_copy.restype = ctypes.c_int
     lib.cq_probe_copy.argtypes = [vp, vp, ctypes.c_size_t, vp]
     lib.cq_probe_mfma.restype = ctypes.c_int
@@ -1046,3 +1065,209 @@ def cq_probe_mfma(a, b, stream=None):
     if st != CQ_OK:
         raise CQError(st, "cq_probe_mfma")
     return d
+
+
+# ---------------------------------------------------------------- caches that stay bounded
+
+def _same_device(*tensors) -> None:
+    """All on the current device (the library launches there, on a stream of that device)."""
+    import torch
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
+
+
+def _check_caches(fmt: CQFormat, batch: int, t_cap: int, pages, *caches) -> None:
+    """uint8 caches (or pools) large enough for the call; the block table has a row for every sequence."""
+    import torch
+    need = cq_paged_cache_bytes(fmt, pages.n_pages) if pages is not None else cq_cache_bytes(fmt, batch, t_cap)
+    if need == 0:
+        raise CQError(CQ_ERR_INVALID_ARG, "cq_cache_bytes")
+    for t in caches:
+        _dev(t, torch.uint8, "code cache")
+        if not t.is_contiguous() or t.numel() < need:
+            raise ValueError("code caches must be contiguous and as large as the format, batch and capacity need")
+    if pages is not None and pages.block_table.shape[0] < batch:
+        raise ValueError("block table has fewer rows than the batch")
+
+
+def _check_seq_lens(seq_lens, batch: int):
+    import torch
+    if seq_lens is None:
+        return None
+    _dev(seq_lens, torch.int32, "seq_lens")
+    if tuple(seq_lens.shape) != (batch,) or not seq_lens.is_contiguous():
+        raise ValueError("seq_lens must be contiguous int32 [B]")
+    return seq_lens.data_ptr()
+
+
+def _check_out(out, shape, device):
+    import torch
+    if out is None:
+        return torch.empty(shape, dtype=torch.float16, device=device)
+    _dev(out, torch.float16, "out")
+    if tuple(out.shape) != tuple(shape) or not out.is_contiguous():
+        raise ValueError(f"out must be contiguous {list(shape)}")
+    return out
+
+
+def _check_weights(weights, batch: int, fmt: CQFormat, t: int, what: str = "weights") -> int:
+    """fp32 [B, n_kv_heads, stride >= t], streams one behind the other; returns the stride."""
+    import torch
+    _dev(weights, torch.float32, what)
+    if weights.dim() != 3 or tuple(weights.shape[:2]) != (batch, fmt.n_kv_heads) or not weights.is_contiguous():
+        raise ValueError(f"{what} must be contiguous fp32 [B, n_kv_heads, tokens]")
+    if weights.shape[2] < t:
+        raise ValueError(f"{what} must hold t tokens per KV head")
+    return int(weights.shape[2])
+
+
+def _workspace(workspace, nbytes: int, device, what: str):
+    import torch
+    if workspace is None:
+        if nbytes == 0:
+            raise CQError(CQ_ERR_INVALID_ARG, what)
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _dev(workspace, torch.uint8, "workspace")
+
+
+def _decode_tensors(q, k_codes, v_codes, k_centroids, v_centroids, fmt: CQFormat, t_cap: int, pages, seq_lens, out):
+    """The checks that the decode calls of this section share; returns (batch, n_q_heads, seq_lens pointer, out)."""
+    import torch
+    _dev(q, torch.float16, "q")
+    if q.dim() != 3 or not q.is_contiguous() or q.shape[2] != fmt.head_dim:
+        raise ValueError("q must be contiguous [B, Hq, head_dim]")
+    batch, n_q_heads = int(q.shape[0]), int(q.shape[1])
+    _check_centroids(fmt, k_centroids, v_centroids)
+    _check_caches(fmt, batch, t_cap, pages, k_codes, v_codes)
+    sl = _check_seq_lens(seq_lens, batch)
+    out = _check_out(out, (batch, n_q_heads, fmt.head_dim), q.device)
+    _same_device(q, k_codes, v_codes, k_centroids, v_centroids, seq_lens, out, None if pages is None else pages.block_table)
+    return batch, n_q_heads, sl, out
+
+
+def cq_decode_window_default_split(fmt: CQFormat, batch: int, n_q_heads: int, t: int, window: int, n_sink: int = 0) -> int:
+    return int(load().cq_decode_window_default_split(ctypes.byref(fmt._c()), batch, n_q_heads, t, window, n_sink))
+
+
+def cq_decode_window_workspace_bytes(fmt: CQFormat, batch: int, n_q_heads: int, t: int, window: int, n_sink: int = 0,
+                                     tokens_per_split: int = 0) -> int:
+    return int(load().cq_decode_window_workspace_bytes(ctypes.byref(fmt._c()), batch, n_q_heads, t, window, n_sink, tokens_per_split))
+
+
+def prepare_decode_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int,
+                                    window: int, n_sink: int = 0, pages=None, seq_lens=None, tokens_per_split: int = 0, out=None,
+                                    workspace=None, x_k_new=None, x_v_new=None):
+    """Check and marshal the arguments of cq_decode_attention_window once (with `pages`, of its paged form; with the new
+    token's rows, of cq_decode_step_window).  Returns (call, out)."""
+    import torch
+    batch, n_q_heads, sl, out = _decode_tensors(q, k_codes, v_codes, k_centroids, v_centroids, fmt, t_cap, pages, seq_lens, out)
+    workspace = _workspace(workspace, cq_decode_window_workspace_bytes(fmt, batch, n_q_heads, t, window, n_sink, tokens_per_split),
+                           q.device, "cq_decode_window_workspace_bytes")
+    f = fmt._c()
+    args = (k_codes.data_ptr(), v_codes.data_ptr(), k_centroids.data_ptr(), v_centroids.data_ptr(), float(scale), ctypes.byref(f),
+            batch, n_q_heads, t, t_cap if pages is None else ctypes.byref(pages._c), sl, window, n_sink, tokens_per_split,
+            out.data_ptr(), workspace.data_ptr(), workspace.numel())
+    name = "cq_decode_attention_window"
+    head = (q.data_ptr(),)
+    if x_k_new is not None or x_v_new is not None:
+        for what, x in (("x_k_new", x_k_new), ("x_v_new", x_v_new)):
+            _dev(x, torch.float16, what)
+            if x.dim() != 2 or tuple(x.shape) != (batch, fmt.channels) or x.stride(1) != 1:
+                raise ValueError(f"{what} must be [B, D] with contiguous rows")
+        if x_k_new.stride(0) != x_v_new.stride(0):
+            raise ValueError("x_k_new and x_v_new must have the same row stride")
+        name = "cq_decode_step_window"
+        head += (x_k_new.data_ptr(), x_v_new.data_ptr(), x_k_new.stride(0))
+    _same_device(workspace, x_k_new, x_v_new)
+    name += "" if pages is None else "_paged"
+    keep = (q, k_codes, v_codes, k_centroids, v_centroids, seq_lens, out, workspace, f, pages, x_k_new, x_v_new)
+    return PreparedCall(getattr(load(), name), head + args, keep, name), out
+
+
+def cq_decode_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int,
+                               window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None,
+                               stream=None):
+    """cq_decode_attention through a sliding window: the last `window` tokens of each sequence and its first `n_sink`."""
+    call, out = prepare_decode_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t, t_cap, window, n_sink,
+                                                None, seq_lens, tokens_per_split, out, workspace)
+    call(stream)
+    return out
+
+
+def cq_decode_attention_window_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
+                                     pages: PageTable, window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0,
+                                     out=None, workspace=None, stream=None):
+    """cq_decode_attention_window over paged pools (pages outside the window and the sinks are not looked at)."""
+    call, out = prepare_decode_attention_window(q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0, window, n_sink,
+                                                pages, seq_lens, tokens_per_split, out, workspace)
+    call(stream)
+    return out
+
+
+def cq_decode_step_window(q, x_k_new, x_v_new, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
+                          t_cap: int, window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0, out=None,
+                          workspace=None, stream=None):
+    """cq_decode_step through a sliding window with sinks: the new token is encoded at position t - 1 (seq_lens[n] - 1)."""
+    if x_k_new is None or x_v_new is None:
+        raise TypeError("x_k_new and x_v_new must be CUDA/HIP tensors")
+    call, out = prepare_decode_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t, t_cap, window, n_sink,
+                                                None, seq_lens, tokens_per_split, out, workspace, x_k_new, x_v_new)
+    call(stream)
+    return out
+
+
+def cq_decode_step_window_paged(q, x_k_new, x_v_new, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
+                                pages: PageTable, window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0, out=None,
+                                workspace=None, stream=None):
+    """cq_decode_step_window over paged pools."""
+    if x_k_new is None or x_v_new is None:
+        raise TypeError("x_k_new and x_v_new must be CUDA/HIP tensors")
+    call, out = prepare_decode_attention_window(q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0, window, n_sink,
+                                                pages, seq_lens, tokens_per_split, out, workspace, x_k_new, x_v_new)
+    call(stream)
+    return out
+
+
+def cq_decode_weights_workspace_bytes(fmt: CQFormat, batch: int, n_q_heads: int, t: int, tokens_per_split: int = 0) -> int:
+    return int(load().cq_decode_weights_workspace_bytes(ctypes.byref(fmt._c()), batch, n_q_heads, t, tokens_per_split))
+
+
+def prepare_decode_attention_weights(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int,
+                                     weights, decay: float = 1.0, pages=None, seq_lens=None, tokens_per_split: int = 0, out=None,
+                                     workspace=None):
+    """Check and marshal the arguments of cq_decode_attention_weights (with `pages`, of its paged form) once.  Returns (call, out)."""
+    batch, n_q_heads, sl, out = _decode_tensors(q, k_codes, v_codes, k_centroids, v_centroids, fmt, t_cap, pages, seq_lens, out)
+    stride = _check_weights(weights, batch, fmt, t)
+    workspace = _workspace(workspace, cq_decode_weights_workspace_bytes(fmt, batch, n_q_heads, t, tokens_per_split), q.device,
+                           "cq_decode_weights_workspace_bytes")
+    _same_device(weights, workspace)
+    f = fmt._c()
+    args = (q.data_ptr(), k_codes.data_ptr(), v_codes.data_ptr(), k_centroids.data_ptr(), v_centroids.data_ptr(), float(scale),
+            ctypes.byref(f), batch, n_q_heads, t, t_cap if pages is None else ctypes.byref(pages._c), sl, tokens_per_split,
+            weights.data_ptr(), stride, float(decay), out.data_ptr(), workspace.data_ptr(), workspace.numel())
+    name = "cq_decode_attention_weights" + ("" if pages is None else "_paged")
+    keep = (q, k_codes, v_codes, k_centroids, v_centroids, seq_lens, weights, out, workspace, f, pages)
+    return PreparedCall(getattr(load(), name), args, keep, name), out
+
+
+def cq_decode_attention_weights(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int,
+                                weights, decay: float = 1.0, seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None,
+                                stream=None):
+    """cq_decode_attention that also adds each cached token's attention weight, summed over the query heads of its KV head, to
+    `weights` fp32 [B, n_kv_heads, tokens]: weights = decay weights + this step's (decay 0: weights are not read)."""
+    call, out = prepare_decode_attention_weights(q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t, t_cap, weights, decay,
+                                                 None, seq_lens, tokens_per_split, out, workspace)
+    call(stream)
+    return out
+
+
+def cq_decode_attention_weights_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
+                                      pages: PageTable, weights, decay: float = 1.0, seq_lens=None, tokens_per_split: int = 0,
+                                      out=None, workspace=None, stream=None):
+    """cq_decode_attention_weights over paged pools."""
+    call, out = prepare_decode_attention_weights(q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0, weights, decay,
+                                                 pages, seq_lens, tokens_per_split, out, workspace)
+    call(stream)
+    return out

@@ -462,6 +462,31 @@ struct TokenView {
     int seq_len_shift, seq_len_floor;
 };
 
+// A sliding window with sinks as the callers give it (window 0: none).  Values beyond the context mean the context.
+struct Window {
+    int window, n_sink;
+};
+cq_status check_window(Window* w, int32_t t)
+{
+    if (w->window <= 0 || w->n_sink < 0) return CQ_ERR_INVALID_ARG;
+    w->window = std::min(w->window, t);
+    w->n_sink = std::min(w->n_sink, t);
+    return CQ_OK;
+}
+
+// The accumulators of attention weights [batch][n_kv_heads][stride].
+struct Weights {
+    float* acc;
+    int64_t stride;
+    float decay;
+};
+cq_status check_weights(const Weights& w, int32_t t)
+{
+    if (!w.acc || !aligned16(w.acc) || w.stride < t || !std::isfinite(w.decay)) return CQ_ERR_INVALID_ARG;
+    return CQ_OK;
+}
+size_t round256(size_t n) { return (n + 255) & ~size_t{255}; }
+
 cq_status decode_common(const void* q, const void* x_k_new, const void* x_v_new, int64_t x_row_stride,
                         const void* k_codes, const void* v_codes,
                         const void* k_centroids, const void* v_centroids,
@@ -471,7 +496,7 @@ cq_status decode_common(const void* q, const void* x_k_new, const void* x_v_new,
                         void* out, void* workspace, size_t workspace_bytes, void* stream, bool step,
                         const void* rope_table = nullptr, int32_t rope_positions = 0,
                         const LayerPtrs* layers = nullptr, int32_t n_layers = 1, const TokenView* view = nullptr,
-                        bool static_scratch = false)
+                        bool static_scratch = false, const Window* window = nullptr, const Weights* weights = nullptr)
 {
     Derived f;
     cq_status st = derive(fmt, &f);
@@ -510,19 +535,24 @@ cq_status decode_common(const void* q, const void* x_k_new, const void* x_v_new,
         if (!rope_table || !aligned16(rope_table)) return CQ_ERR_INVALID_ARG;
         if (rope_positions < 0 || rope_positions % kTileTokens != 0 || t > rope_positions) return CQ_ERR_INVALID_ARG;
     }
+    Window win = window ? *window : Window{0, 0};
+    if (window && (st = check_window(&win, t)) != CQ_OK) return st;
+    if (weights && (st = check_weights(*weights, t)) != CQ_OK) return st;
     const int max_tiles = rope ? decode_rope_max_tiles_per_split() : decode_max_tiles_per_split(f);
+    const int n_tiles = view_tiles(t, 1, win.window, win.n_sink);
     const int tiles = tokens_per_split ? tokens_per_split / kTileTokens
                                        : (rope ? rope_default_tiles_per_split(f, batch, n_q_heads, t)
-                                               : default_tiles_per_split(f, batch, n_q_heads, t, max_tiles));
+                                               : default_tiles_per_split(f, batch, n_q_heads, window ? n_tiles * kTileTokens : t, max_tiles));
     if (tiles > max_tiles) return CQ_ERR_INVALID_ARG;
-    const int n_tiles = (t + kTileTokens - 1) / kTileTokens;
     const int n_split = (n_tiles + tiles - 1) / tiles;
-    const size_t need = sizeof(float) * (size_t)batch * n_q_heads * n_split * (f.head_dim + kPartialHeader) * n_layers;
+    size_t need = sizeof(float) * (size_t)batch * n_q_heads * n_split * (f.head_dim + kPartialHeader) * n_layers;
+    const size_t stats_at = round256(need), scores_at = stats_at + round256(sizeof(float2) * (size_t)batch * n_q_heads * n_split);
+    if (weights) need = scores_at + sizeof(float) * (size_t)batch * n_q_heads * n_tiles * kTileTokens;
     if (workspace_bytes < need) return CQ_ERR_WORKSPACE_TOO_SMALL;
     if ((int64_t)batch * n_q_heads * n_split * n_layers > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
     if (static_scratch && g_static_scratch.get(&workspace) != hipSuccess) return CQ_ERR_HIP;
 
-    DecodeArgs a;
+    DecodeViewArgs a;
     a.layers = layers;
     a.n_layers = n_layers;
     a.wgs_per_layer = batch * n_q_heads * n_split;
@@ -551,7 +581,16 @@ cq_status decode_common(const void* q, const void* x_k_new, const void* x_v_new,
     a.seq_len_floor = view ? view->seq_len_floor : 1;
     a.merge_counters = nullptr;
     a.f = f;
+    a.window = win.window;
+    a.n_sink = win.n_sink;
+    a.scores = weights ? reinterpret_cast<float*>(static_cast<char*>(workspace) + scores_at) : nullptr;
+    a.stats = weights ? reinterpret_cast<float2*>(static_cast<char*>(workspace) + stats_at) : nullptr;
+    a.score_stride = (int64_t)n_tiles * kTileTokens;
+    a.weights = weights ? weights->acc : nullptr;
+    a.weights_stride = weights ? weights->stride : 0;
+    a.decay = weights ? weights->decay : 0.f;
     if (rope) return launch_decode_rope(a, static_cast<const float*>(rope_table), rope_positions, static_cast<hipStream_t>(stream));
+    if (window || weights) return launch_decode_view(a, static_cast<hipStream_t>(stream));
     return launch_decode(a, static_cast<hipStream_t>(stream));
 }
 
@@ -618,6 +657,108 @@ cq_status cq_decode_step_paged(const void* q, const void* x_k_new, const void* x
     return decode_common(q, x_k_new, x_v_new, x_row_stride, k_pool, v_pool, k_centroids, v_centroids, scale, fmt,
                          batch, n_q_heads, t, 0, pages, seq_lens, tokens_per_split, out, workspace, workspace_bytes,
                          stream, true);
+}
+
+int32_t cq_decode_window_default_split(const cq_format* fmt, int32_t batch, int32_t n_q_heads, int32_t t, int32_t window, int32_t n_sink)
+{
+    Window w{window, n_sink};
+    if (t <= 0 || check_window(&w, t) != CQ_OK) return 0;
+    return cq_decode_default_split(fmt, batch, n_q_heads, view_tiles(t, 1, w.window, w.n_sink) * kTileTokens);
+}
+
+size_t cq_decode_window_workspace_bytes(const cq_format* fmt, int32_t batch, int32_t n_q_heads, int32_t t, int32_t window, int32_t n_sink,
+                                        int32_t tokens_per_split)
+{
+    Window w{window, n_sink};
+    if (t <= 0 || check_window(&w, t) != CQ_OK) return 0;
+    return cq_decode_workspace_bytes(fmt, batch, n_q_heads, view_tiles(t, 1, w.window, w.n_sink) * kTileTokens, tokens_per_split);
+}
+
+cq_status cq_decode_attention_window(const void* q, const void* k_codes, const void* v_codes,
+                                     const void* k_centroids, const void* v_centroids,
+                                     float scale, const cq_format* fmt,
+                                     int32_t batch, int32_t n_q_heads, int32_t t, int32_t t_cap,
+                                     const int32_t* seq_lens, int32_t window, int32_t n_sink, int32_t tokens_per_split,
+                                     void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const Window w{window, n_sink};
+    return decode_common(q, nullptr, nullptr, 0, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, batch, n_q_heads, t, t_cap, nullptr,
+                         seq_lens, tokens_per_split, out, workspace, workspace_bytes, stream, false, nullptr, 0, nullptr, 1, nullptr, false, &w);
+}
+
+cq_status cq_decode_attention_window_paged(const void* q, const void* k_pool, const void* v_pool,
+                                           const void* k_centroids, const void* v_centroids,
+                                           float scale, const cq_format* fmt,
+                                           int32_t batch, int32_t n_q_heads, int32_t t, const cq_page_table* pages,
+                                           const int32_t* seq_lens, int32_t window, int32_t n_sink, int32_t tokens_per_split,
+                                           void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!pages) return CQ_ERR_INVALID_ARG;
+    const Window w{window, n_sink};
+    return decode_common(q, nullptr, nullptr, 0, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, batch, n_q_heads, t, 0, pages,
+                         seq_lens, tokens_per_split, out, workspace, workspace_bytes, stream, false, nullptr, 0, nullptr, 1, nullptr, false, &w);
+}
+
+cq_status cq_decode_step_window(const void* q, const void* x_k_new, const void* x_v_new, int64_t x_row_stride,
+                                void* k_codes, void* v_codes,
+                                const void* k_centroids, const void* v_centroids,
+                                float scale, const cq_format* fmt,
+                                int32_t batch, int32_t n_q_heads, int32_t t, int32_t t_cap,
+                                const int32_t* seq_lens, int32_t window, int32_t n_sink, int32_t tokens_per_split,
+                                void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const Window w{window, n_sink};
+    return decode_common(q, x_k_new, x_v_new, x_row_stride, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, batch, n_q_heads, t, t_cap,
+                         nullptr, seq_lens, tokens_per_split, out, workspace, workspace_bytes, stream, true, nullptr, 0, nullptr, 1, nullptr, false, &w);
+}
+
+cq_status cq_decode_step_window_paged(const void* q, const void* x_k_new, const void* x_v_new, int64_t x_row_stride,
+                                      void* k_pool, void* v_pool,
+                                      const void* k_centroids, const void* v_centroids,
+                                      float scale, const cq_format* fmt,
+                                      int32_t batch, int32_t n_q_heads, int32_t t, const cq_page_table* pages,
+                                      const int32_t* seq_lens, int32_t window, int32_t n_sink, int32_t tokens_per_split,
+                                      void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!pages) return CQ_ERR_INVALID_ARG;
+    const Window w{window, n_sink};
+    return decode_common(q, x_k_new, x_v_new, x_row_stride, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, batch, n_q_heads, t, 0,
+                         pages, seq_lens, tokens_per_split, out, workspace, workspace_bytes, stream, true, nullptr, 0, nullptr, 1, nullptr, false, &w);
+}
+
+size_t cq_decode_weights_workspace_bytes(const cq_format* fmt, int32_t batch, int32_t n_q_heads, int32_t t, int32_t tokens_per_split)
+{
+    const size_t partials = cq_decode_workspace_bytes(fmt, batch, n_q_heads, t, tokens_per_split);
+    if (partials == 0) return 0;
+    const size_t rows = (size_t)batch * n_q_heads, splits = partials / (sizeof(float) * (fmt->head_dim + kPartialHeader));
+    return round256(partials) + round256(sizeof(float2) * splits) + sizeof(float) * rows * (((size_t)t + kTileTokens - 1) / kTileTokens * kTileTokens);
+}
+
+cq_status cq_decode_attention_weights(const void* q, const void* k_codes, const void* v_codes,
+                                      const void* k_centroids, const void* v_centroids,
+                                      float scale, const cq_format* fmt,
+                                      int32_t batch, int32_t n_q_heads, int32_t t, int32_t t_cap,
+                                      const int32_t* seq_lens, int32_t tokens_per_split,
+                                      float* weights, int64_t weights_stride, float decay,
+                                      void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const Weights w{weights, weights_stride, decay};
+    return decode_common(q, nullptr, nullptr, 0, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, batch, n_q_heads, t, t_cap, nullptr,
+                         seq_lens, tokens_per_split, out, workspace, workspace_bytes, stream, false, nullptr, 0, nullptr, 1, nullptr, false, nullptr, &w);
+}
+
+cq_status cq_decode_attention_weights_paged(const void* q, const void* k_pool, const void* v_pool,
+                                            const void* k_centroids, const void* v_centroids,
+                                            float scale, const cq_format* fmt,
+                                            int32_t batch, int32_t n_q_heads, int32_t t, const cq_page_table* pages,
+                                            const int32_t* seq_lens, int32_t tokens_per_split,
+                                            float* weights, int64_t weights_stride, float decay,
+                                            void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!pages) return CQ_ERR_INVALID_ARG;
+    const Weights w{weights, weights_stride, decay};
+    return decode_common(q, nullptr, nullptr, 0, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, batch, n_q_heads, t, 0, pages,
+                         seq_lens, tokens_per_split, out, workspace, workspace_bytes, stream, false, nullptr, 0, nullptr, 1, nullptr, false, nullptr, &w);
 }
 
 namespace {

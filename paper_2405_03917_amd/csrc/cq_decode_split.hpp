@@ -14,6 +14,57 @@ constexpr int kDecodeWaves = kDecodeThreads / 64;
 constexpr int kChunkTiles8 = 16;
 constexpr int kChunkTiles10 = 32;
 
+// What a call sees of a sequence, and what it returns besides the output.
+enum View : int {
+    kWhole = 0,         // every token
+    kWindow = 1,        // the last `window` tokens and the first n_sink
+    kScores = 2,        // every token, and the scores go to memory
+};
+
+// The tiles of a sequence that a call walks, numbered without gaps: of a window, the sinks' tiles in front of it (`head`
+// of them), then its own, `skip` tiles further on in the cache.  Every tile of the view holds a token that is seen.
+template <int VIEW>
+struct Seen {
+    int n_tiles;
+    __device__ __forceinline__ Seen() = default;
+    __device__ __forceinline__ Seen(const DecodeArgs&, int t_n) : n_tiles((t_n + kTileTokens - 1) / kTileTokens) {}
+    __device__ __forceinline__ int tile(int i) const { return i; }
+    __device__ __forceinline__ bool edge(int i) const { return i == n_tiles - 1; }      // tiles that hold tokens not seen
+    __device__ __forceinline__ bool token(int tok, int t_n) const { return tok < t_n; }
+};
+template <>
+struct Seen<kWindow> {
+    int n_tiles, head, skip, first, n_sink;             // first: the window's first token
+    __device__ __forceinline__ Seen() = default;
+    __device__ __forceinline__ Seen(const DecodeViewArgs& a, int t_n)
+    {
+        n_sink = a.n_sink;
+        first = max(0, t_n - a.window);
+        const int at = first / kTileTokens;
+        head = min((n_sink + kTileTokens - 1) / kTileTokens, at);
+        skip = at - head;
+        n_tiles = (t_n + kTileTokens - 1) / kTileTokens - skip;
+    }
+    __device__ __forceinline__ int tile(int i) const { return i < head ? i : i + skip; }
+    __device__ __forceinline__ bool edge(int i) const { return i == n_tiles - 1 || i == head || i == head - 1; }
+    __device__ __forceinline__ bool token(int tok, int t_n) const { return tok < t_n && (tok >= first || tok < n_sink); }
+};
+
+// kScores: the score of a row's token to memory.
+template <int VIEW, class Args>
+__device__ __forceinline__ void keep_score(const Args& a, size_t row, int tok, float s)
+{
+    if constexpr (VIEW == kScores) a.scores[row * a.score_stride + tok] = s;
+}
+
+// kScores: a split's reference and sum.  (The sum of the probabilities in fixed point, by which the output is divided, is no
+// substitute: equal probabilities of a long context are all rounded the same way, 1e-4 of their sum at 131072 tokens.)
+template <int VIEW, class Args>
+__device__ __forceinline__ void keep_stats(const Args& a, size_t row, int split, float m, float l)
+{
+    if constexpr (VIEW == kScores) a.stats[row * a.n_split + split] = make_float2(m, l);
+}
+
 // LayerPtrs as the kernel reads it.  A pointer read from memory could point anywhere (LDS,
 // scratch) as far as the compiler knows, and every access through it would be a flat instruction,
 // which waits on the LDS counter and the memory counter at once; the table's pointers are

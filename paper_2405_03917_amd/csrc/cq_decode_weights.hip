@@ -1,0 +1,87 @@
+// Attention weights added up per cached token (cq_decode_attention_weights), for gfx950: what follows the attention
+// kernel, which left every score of the call (base 2) and, per context split, the softmax reference m and sum l.
+//
+//   weights[n][h][i] = decay weights[n][h][i] + sum over the query heads q of KV head h of 2^(s_q,i - M_q) / L_q,
+//   M_q = max over splits of m, L_q = sum over splits of l 2^(m - M_q)
+//
+// A weight needs the sum over the whole context, which no workgroup of the attention kernel has while others still run,
+// and with grouped queries a token's sum runs over workgroups; hence a second launch, which merges the output's
+// splits too.  Every sum is formed by one thread in a fixed order: no atomics, equal calls give equal bits.
+// Bound by memory: 4 bytes a query head and token (the scores, mostly still in the caches) and 8 a KV head and token.
+#include "cq_decode_split.hpp"
+
+namespace cq {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTokensPerThread = 4;
+constexpr int kTokens = kThreads * kTokensPerThread;
+
+__global__ __launch_bounds__(kThreads) void decode_weights_kernel(DecodeViewArgs a, int merge_wgs, int blocks)
+{
+    extern __shared__ float2 stats[];                       // (M, 1 / L) per query head of the KV head
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int D = a.f.head_dim, part = D + kPartialHeader;
+    if ((int)blockIdx.x < merge_wgs) {                      // two rows of the output
+        const int row = 2 * blockIdx.x + (tid >> 7);
+        if (row < a.batch * a.n_q_heads)
+            merge_splits<false>(a.partials + (size_t)row * a.n_split * part, a.n_split, D,
+                                a.out + (size_t)(row / a.n_q_heads) * a.out_batch_stride + (size_t)(row % a.n_q_heads) * D, tid & 127, 128);
+        return;
+    }
+    const int idx = blockIdx.x - merge_wgs;
+    const int block = idx % blocks, stream = idx / blocks;
+    const int n = stream / a.f.n_kv_heads, hkv = stream % a.f.n_kv_heads;
+    const int qper = a.n_q_heads / a.f.n_kv_heads;
+    int t_n = a.t;
+    if (a.seq_lens) t_n = min(max(a.seq_lens[n], 1), a.t);
+    const int first = block * kTokens;
+    if (first >= t_n) return;
+    const size_t row0 = (size_t)n * a.n_q_heads + (size_t)hkv * qper;
+    for (int h = wave; h < qper; h += kThreads / 64) {
+        const float2* p = a.stats + (row0 + h) * a.n_split;
+        float m = -INFINITY;
+        for (int s = lane; s < a.n_split; s += 64) m = fmaxf(m, p[s].x);
+        m = wave_max(m);
+        float l = 0.f;
+        for (int s = lane; s < a.n_split; s += 64) l = __builtin_fmaf(p[s].y, __builtin_amdgcn_exp2f(p[s].x - m), l);
+        l = wave_sum(l);
+        if (lane == 0) stats[h] = make_float2(m, 1.f / l);
+    }
+    __syncthreads();
+    float* acc = a.weights + (size_t)stream * a.weights_stride;
+    float old[kTokensPerThread], w[kTokensPerThread];
+#pragma unroll
+    for (int k = 0; k < kTokensPerThread; ++k) {
+        const int tok = first + k * kThreads + tid;
+        old[k] = a.decay != 0.f && tok < t_n ? acc[tok] : 0.f;      // (without decay the accumulators are not read)
+        w[k] = 0.f;
+    }
+    for (int h = 0; h < qper; ++h) {
+        const float* s = a.scores + (row0 + h) * a.score_stride + first + tid;
+        const float2 st = stats[h];
+#pragma unroll
+        for (int k = 0; k < kTokensPerThread; ++k)
+            if (first + k * kThreads + tid < t_n) w[k] = __builtin_fmaf(__builtin_amdgcn_exp2f(s[k * kThreads] - st.x), st.y, w[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kTokensPerThread; ++k) {
+        const int tok = first + k * kThreads + tid;
+        if (tok < t_n) acc[tok] = __builtin_fmaf(a.decay, old[k], w[k]);
+    }
+}
+
+}  // namespace
+
+cq_status launch_decode_weights(const DecodeViewArgs& a, hipStream_t stream)
+{
+    const int qper = a.n_q_heads / a.f.n_kv_heads;
+    const int blocks = (a.t + kTokens - 1) / kTokens;
+    const int merge_wgs = a.n_split > 1 ? (a.batch * a.n_q_heads + 1) / 2 : 0;
+    const int64_t grid = (int64_t)merge_wgs + (int64_t)a.batch * a.f.n_kv_heads * blocks;
+    if (grid > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
+    hipLaunchKernelGGL(decode_weights_kernel, dim3((unsigned)grid), dim3(kThreads), sizeof(float2) * (size_t)qper, stream, a, merge_wgs, blocks);
+    return hipGetLastError() == hipSuccess ? CQ_OK : CQ_ERR_HIP;
+}
+
+}  // namespace cq

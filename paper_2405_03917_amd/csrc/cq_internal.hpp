@@ -129,6 +129,30 @@ struct DecodeArgs {
     Derived f;
 };
 
+// ... of a call that sees a window of each sequence, or wants its attention weights.
+struct DecodeViewArgs : DecodeArgs {
+    // sliding window (0: none): a query at position p sees tokens p - window + 1 .. p and 0 .. n_sink - 1
+    int window, n_sink;
+    // attention weights wanted (else null): every score, base 2, goes to scores[row (sequence, query head)][token] with
+    // score_stride tokens a row, and from there to the accumulators weights[sequence][KV head][token]
+    float* scores;
+    int64_t score_stride;
+    float2* stats;            // [row][n_split]: the softmax reference and the fp32 sum of 2^(score - reference) of a split
+    float* weights;
+    int64_t weights_stride;
+    float decay;
+};
+
+// Tiles of a context of up to t tokens that m query tokens look at through a window with sinks (0: all of it): the
+// sinks' tiles, and the most that window + m - 1 neighbouring tokens can touch.
+inline int view_tiles(int t, int m, int window, int n_sink)
+{
+    const int all = (t + kTileTokens - 1) / kTileTokens;
+    if (window <= 0) return all;
+    const int64_t seen = ((int64_t)n_sink + kTileTokens - 1) / kTileTokens + ((int64_t)window + m + kTileTokens - 3) / kTileTokens + 1;
+    return seen < all ? (int)seen : all;
+}
+
 // Causal attention of the last m tokens of every sequence over its cache (cq_chunk.hip).
 struct ChunkArgs {
     const uint16_t* q;        // fp16 [batch][m][n_q_heads][head_dim]
@@ -205,6 +229,10 @@ cq_status launch_encode(const EncodeArgs& a, hipStream_t stream);
 // many tokens per sequence: the MFMA-filtered kernel (cq_encode_mfma.hip)
 cq_status launch_encode_tiles(const EncodeArgs& a, hipStream_t stream);
 cq_status launch_decode(const DecodeArgs& a, hipStream_t stream);
+cq_status launch_decode_view(const DecodeViewArgs& a, hipStream_t stream);
+// cq_decode_weights.hip: behind an attention kernel that wrote scores and partials, the accumulators, and (several splits)
+// the merged rows of the output
+cq_status launch_decode_weights(const DecodeViewArgs& a, hipStream_t stream);
 // grouped queries, two query heads per workgroup (cq_decode_pair.hip): whether a call goes there, and the launch
 bool decode_takes_pairs(const DecodeArgs& a);
 int decode_pair_chunk_tiles(const DecodeArgs& a);
@@ -214,10 +242,13 @@ struct DecodePlan {
 };
 DecodePlan decode_plan(const DecodeArgs& a);
 cq_status launch_decode_pair(const DecodeArgs& a, hipStream_t stream);
+cq_status launch_decode_pair_view(const DecodeViewArgs& a, hipStream_t stream);
 // grouped queries, up to four query heads per workgroup, both codebooks in LDS (cq_decode_quad.hip): whether a call goes
-// there, and its arguments with neighbouring splits joined; the launch of those; that of keys cached before RoPE
-bool decode_takes_quads(const DecodeArgs& a, DecodeArgs* joined);
+// there (a context of n_tiles tiles), and its arguments with neighbouring splits joined; the launch of those; that of
+// keys cached before RoPE
+bool decode_takes_quads(const DecodeArgs& a, int n_tiles, DecodeArgs* joined);
 cq_status launch_decode_quad(const DecodeArgs& joined, hipStream_t stream);
+cq_status launch_decode_quad_view(const DecodeViewArgs& joined, hipStream_t stream);
 cq_status launch_decode_quad_rope(const DecodeArgs& a, const float2* tile_tab, const float2* lane_tab, hipStream_t stream);
 // centroids fp16 [G][2^b][c] of a sub-byte format -> fp16 [G / fuse][256][c fuse] of its fused format
 cq_status launch_expand_codebook(const uint16_t* centroids, const Derived& f, uint16_t* fused, hipStream_t stream);

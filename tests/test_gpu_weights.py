@@ -1,0 +1,110 @@
+"""Decode attention that adds up attention weights: the output is cq_decode_attention's to its tolerance, the accumulators
+follow the 64-bit definition to the derived bound, and nothing else is written."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2405_03917_amd as cq
+from bounded_util import FORMATS, SCALE, Cache, attention, queries, weight_tolerance
+from gpu_util import check_attention
+
+pytestmark = pytest.mark.gpu
+
+
+def _run(cache, q, t, weights, decay, lens=None, paged=False, split=0):
+    sl = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    if paged:
+        return cq.cq_decode_attention_weights_paged(q, *cache.pools, cache.ck, cache.cv, SCALE, cache.fmt, t, cache.pages(), weights,
+                                                    decay, sl, split)
+    return cq.cq_decode_attention_weights(q, cache.k, cache.v, cache.ck, cache.cv, SCALE, cache.fmt, t, cache.t_cap, weights, decay,
+                                          sl, split)
+
+
+def _check(cache, q, out, before, after, decay, lens):
+    ref, sums, largest = attention(cache, q[:, None], lens)
+    check_attention(out.cpu().numpy(), ref[:, 0].numpy())
+    old, got = before.double().cpu(), after.double().cpu()
+    qper = q.shape[1] // cache.fmt.n_kv_heads
+    for n, length in enumerate(lens):
+        kept = decay * old[n, :, :length] if decay else torch.zeros_like(old[n, :, :length])
+        want = kept + sums[n, :, :length]
+        # (2^-23 of the old accumulator: its product and sum; 2^-126: below, fp32 has fewer digits)
+        room = weight_tolerance(largest, qper) * sums[n, :, :length] + 2.0 ** -23 * (kept.abs() + want.abs()) + 2.0 ** -126
+        assert ((got[n, :, :length] - want).abs() <= room).all()
+        assert torch.equal(after[n, :, length:], before[n, :, length:])
+
+
+SIZES = [(1, 8, 8, 1), (2, 4, 2, 64), (1, 32, 32, 2000), (16, 32, 16, 1500), (18, 32, 8, 300), (40, 8, 2, 2100), (3, 6, 2, 5000), (2, 2, 2, 20001)]
+
+
+@pytest.mark.parametrize("c,b", FORMATS)
+@pytest.mark.parametrize("batch,hq,hkv,t", SIZES)
+def test_weights(c, b, batch, hq, hkv, t):
+    cap = -(-t // 64) * 64
+    cache = Cache(c, b, hkv, batch, cap, seed=t + batch)
+    rng = np.random.default_rng(t)
+    lens = [t] + [int(x) for x in rng.integers(1, t + 1, batch - 1)]
+    q = queries((batch, hq, 128), t)
+    for decay, extra, paged in ((1.0, 0, False), (0.5, 3, True)):
+        weights = torch.rand(batch, hkv, t + extra, device="cuda")
+        before = weights.clone()
+        out = _run(cache, q, t, weights, decay, lens, paged)
+        _check(cache, q, out, before, weights, decay, lens)
+
+
+@pytest.mark.parametrize("c,b", FORMATS)
+def test_without_decay_the_accumulators_are_not_read(c, b):
+    cache = Cache(c, b, 8, 20, 640, seed=c)
+    lens = [600] * 19 + [77]
+    q = queries((20, 32, 128), 2)
+    weights = torch.full((20, 8, 640), float("nan"), device="cuda")
+    out = _run(cache, q, 600, weights, 0.0, lens)
+    _check(cache, q, out, torch.zeros_like(weights), torch.nan_to_num(weights), 0.0, lens)
+    assert torch.isnan(weights[0, :, 600:]).all() and torch.isnan(weights[19, :, 77:]).all()
+
+
+def test_equal_scores_share_the_weight():
+    """A query of zeros: every weight is 1 / t, for which the sum of rounded probabilities would be 1e-4 off."""
+    cache = Cache(8, 8, 2, 1, 131072, seed=1)
+    q = torch.zeros(1, 2, 128, dtype=torch.float16, device="cuda")
+    weights = torch.empty(1, 2, 131072, device="cuda")
+    _run(cache, q, 131072, weights, 0.0)
+    assert ((weights.double() * 131072 - 1).abs() <= 64 * 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("split", [64, 192, 1024])
+@pytest.mark.parametrize("c,b", FORMATS)
+def test_given_splits_and_lengths_that_leave_splits_empty(c, b, split):
+    cache = Cache(c, b, 4, 3, 1600, seed=split)
+    q = queries((3, 8, 128), split, 3.0)
+    lens = [1555, 1, 700]
+    weights = torch.rand(3, 4, 1600, device="cuda")
+    before = weights.clone()
+    out = _run(cache, q, 1555, weights, 0.25, lens, split=split)
+    _check(cache, q, out, before, weights, 0.25, lens)
+
+
+def test_the_same_bits_again_and_captured():
+    cache = Cache(4, 8, 8, 24, 2048, seed=1)
+    q = queries((24, 32, 128), 1)
+    sl = torch.tensor([2000] + list(range(30, 1640, 70)), dtype=torch.int32, device="cuda")
+    start = torch.rand(24, 8, 2048, device="cuda")
+    first = start.clone()
+    out = cq.cq_decode_attention_weights(q, cache.k, cache.v, cache.ck, cache.cv, SCALE, cache.fmt, 2000, 2048, first, 0.5, sl)
+    weights, got = start.clone(), torch.empty_like(out)
+    call, _ = cq.prepare_decode_attention_weights(q, cache.k, cache.v, cache.ck, cache.cv, SCALE, cache.fmt, 2000, 2048, weights, 0.5,
+                                                  seq_lens=sl, out=got)
+    call()
+    torch.cuda.synchronize()
+    assert torch.equal(weights, first) and torch.equal(got, out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(3):
+        weights.copy_(start)
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(weights, first) and torch.equal(got, out)
+        call()
+        torch.cuda.synchronize()
