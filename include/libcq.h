@@ -551,6 +551,28 @@ CQ_API cq_status cq_decode_step_window_paged(const void *q, const void *x_k_new,
                                       void *out, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * cq_chunk_attention_window[_paged] -- cq_chunk_attention[_paged] likewise: query token j, at position p = t_n - m + j, attends to
+ * the tokens i <= p with i > p - window or i < n_sink.  Tiles outside all of a sequence's m windows and its sinks are not
+ * read.  tokens_per_split: 0 = the library's default, otherwise a multiple of 64, of the tokens that are walked.
+ * Chunks of few tokens go where those of cq_chunk_attention over as many tokens would (token by token: bit-identical to
+ * m calls of cq_decode_attention_window).
+ *   workspace         device, cq_chunk_window_workspace_bytes(...) bytes (may be null when that is 0)
+ * Errors: as cq_chunk_attention; CQ_ERR_INVALID_ARG also for window <= 0 or n_sink < 0.
+ */
+CQ_API size_t cq_chunk_window_workspace_bytes(const cq_format *fmt, int32_t batch, int32_t n_q_heads, int32_t m, int32_t t,
+                                       int32_t window, int32_t n_sink, int32_t tokens_per_split);
+CQ_API cq_status cq_chunk_attention_window(const void *q, const void *k_codes, const void *v_codes,
+                                    const void *k_centroids, const void *v_centroids, float scale, const cq_format *fmt,
+                                    int32_t batch, int32_t n_q_heads, int32_t m, int32_t t, int32_t t_cap,
+                                    const int32_t *seq_lens, int32_t window, int32_t n_sink, int32_t tokens_per_split,
+                                    void *out, void *workspace, size_t workspace_bytes, void *stream);
+CQ_API cq_status cq_chunk_attention_window_paged(const void *q, const void *k_pool, const void *v_pool,
+                                          const void *k_centroids, const void *v_centroids, float scale, const cq_format *fmt,
+                                          int32_t batch, int32_t n_q_heads, int32_t m, int32_t t, const cq_page_table *pages,
+                                          const int32_t *seq_lens, int32_t window, int32_t n_sink, int32_t tokens_per_split,
+                                          void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * cq_decode_attention_weights[_paged] -- cq_decode_attention[_paged] that also adds up the attention weights: for every
  * sequence n, KV head h and token i < t (seq_lens[n]),
  *     weights[n][h][i] = decay * weights[n][h][i] + sum over the query heads of h of softmax(scale q.k)_i

@@ -36,6 +36,7 @@ EXPORTS = (
     "cq_chunk_rope_workspace_bytes", "cq_chunk_attention_rope", "cq_chunk_attention_rope_paged",
     "cq_decode_window_default_split", "cq_decode_window_workspace_bytes", "cq_decode_attention_window",
     "cq_decode_attention_window_paged", "cq_decode_step_window", "cq_decode_step_window_paged",
+    "cq_chunk_window_workspace_bytes", "cq_chunk_attention_window", "cq_chunk_attention_window_paged",
     "cq_decode_weights_workspace_bytes", "cq_decode_attention_weights", "cq_decode_attention_weights_paged",
     "cq_probe_stream_read", "cq_probe_copy", "cq_probe_mfma", "cq_probe_decode_plan",
 )
@@ -203,6 +204,11 @@ def load() -> ctypes.CDLL:
     for at, name in ((i32, "cq_decode_step_window"), (pp, "cq_decode_step_window_paged")):
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, f32, fp, i32, i32, i32, at, vp, i32, i32, i32, vp, vp, size, vp]
+    lib.cq_chunk_window_workspace_bytes.restype = size
+    lib.cq_chunk_window_workspace_bytes.argtypes = [fp, i32, i32, i32, i32, i32, i32, i32]
+    for at, name in ((i32, "cq_chunk_attention_window"), (pp, "cq_chunk_attention_window_paged")):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = [vp, vp, vp, vp, vp, f32, fp, i32, i32, i32, i32, at, vp, i32, i32, i32, vp, vp, size, vp]
     lib.cq_decode_weights_workspace_bytes.restype = size
     lib.cq_decode_weights_workspace_bytes.argtypes = [fp, i32, i32, i32, i32]
     for at, name in ((i32, "cq_decode_attention_weights"), (pp, "cq_decode_attention_weights_paged")):
@@ -1226,6 +1232,57 @@ def cq_decode_step_window_paged(q, x_k_new, x_v_new, k_pool, v_pool, k_centroids
         raise TypeError("x_k_new and x_v_new must be CUDA/HIP tensors")
     call, out = prepare_decode_attention_window(q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0, window, n_sink,
                                                 pages, seq_lens, tokens_per_split, out, workspace, x_k_new, x_v_new)
+    call(stream)
+    return out
+
+
+def cq_chunk_window_workspace_bytes(fmt: CQFormat, batch: int, n_q_heads: int, m: int, t: int, window: int, n_sink: int = 0,
+                                    tokens_per_split: int = 0) -> int:
+    return int(load().cq_chunk_window_workspace_bytes(ctypes.byref(fmt._c()), batch, n_q_heads, m, t, window, n_sink, tokens_per_split))
+
+
+def prepare_chunk_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int,
+                                   window: int, n_sink: int = 0, pages=None, seq_lens=None, tokens_per_split: int = 0, out=None,
+                                   workspace=None):
+    """Check and marshal the arguments of cq_chunk_attention_window (with `pages`, of its paged form) once.  Returns (call, out)."""
+    import torch
+    _dev(q, torch.float16, "q")
+    if q.dim() != 4 or not q.is_contiguous() or q.shape[3] != fmt.head_dim:
+        raise ValueError("q must be contiguous [B, m, Hq, head_dim]")
+    batch, m, n_q_heads = int(q.shape[0]), int(q.shape[1]), int(q.shape[2])
+    _check_centroids(fmt, k_centroids, v_centroids)
+    _check_caches(fmt, batch, t_cap, pages, k_codes, v_codes)
+    sl = _check_seq_lens(seq_lens, batch)
+    out = _check_out(out, tuple(q.shape), q.device)
+    workspace = _workspace(workspace, max(16, cq_chunk_window_workspace_bytes(fmt, batch, n_q_heads, m, t, window, n_sink, tokens_per_split)),
+                           q.device, "cq_chunk_window_workspace_bytes")
+    _same_device(q, k_codes, v_codes, k_centroids, v_centroids, seq_lens, out, workspace, None if pages is None else pages.block_table)
+    f = fmt._c()
+    args = (q.data_ptr(), k_codes.data_ptr(), v_codes.data_ptr(), k_centroids.data_ptr(), v_centroids.data_ptr(), float(scale),
+            ctypes.byref(f), batch, n_q_heads, m, t, t_cap if pages is None else ctypes.byref(pages._c), sl, window, n_sink,
+            tokens_per_split, out.data_ptr(), workspace.data_ptr(), workspace.numel())
+    name = "cq_chunk_attention_window" + ("" if pages is None else "_paged")
+    keep = (q, k_codes, v_codes, k_centroids, v_centroids, seq_lens, out, workspace, f, pages)
+    return PreparedCall(getattr(load(), name), args, keep, name), out
+
+
+def cq_chunk_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int,
+                              window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None,
+                              stream=None):
+    """cq_chunk_attention through sliding windows: each of the last m tokens sees the `window` tokens up to its own position
+    and the sequence's first `n_sink`."""
+    call, out = prepare_chunk_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t, t_cap, window, n_sink,
+                                               None, seq_lens, tokens_per_split, out, workspace)
+    call(stream)
+    return out
+
+
+def cq_chunk_attention_window_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
+                                    pages: PageTable, window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0,
+                                    out=None, workspace=None, stream=None):
+    """cq_chunk_attention_window over paged pools."""
+    call, out = prepare_chunk_attention_window(q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0, window, n_sink,
+                                               pages, seq_lens, tokens_per_split, out, workspace)
     call(stream)
     return out
 

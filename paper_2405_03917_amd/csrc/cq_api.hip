@@ -815,25 +815,29 @@ struct TokenCall {
     int t, tiles, n_split;
     size_t workspace;
 };
-TokenCall chunk_token_call(const Derived& f, int batch, int n_q_heads, int m, int t, int j)
+TokenCall chunk_token_call(const Derived& f, int batch, int n_q_heads, int m, int t, int j, Window w = {0, 0})
 {
     TokenCall c;
     c.t = t - (m - 1 - j);
-    c.tiles = default_tiles_per_split(f, batch, n_q_heads, c.t);
-    const int n_tiles = (c.t + kTileTokens - 1) / kTileTokens;
+    const int n_tiles = view_tiles(c.t, 1, w.window, w.n_sink);
+    c.tiles = default_tiles_per_split(f, batch, n_q_heads, w.window ? n_tiles * kTileTokens : c.t);
     c.n_split = (n_tiles + c.tiles - 1) / c.tiles;
     c.workspace = c.n_split > 1 ? sizeof(float) * (size_t)batch * n_q_heads * c.n_split * (f.head_dim + kPartialHeader) : 0;
     return c;
 }
 
+// tokens that a chunk walks: the context, or what its windows and sinks can touch
+int chunk_span(int m, int t, Window w) { return w.window ? view_tiles(t, m, w.window, w.n_sink) * kTileTokens : t; }
+
 // Workspace of a chunk as the library reports it: for the tokens one by one, or for the many-row kernel's split.
-size_t chunk_workspace(const Derived& f, int batch, int n_q_heads, int m, int t, int tokens_per_split)
+size_t chunk_workspace(const Derived& f, int batch, int n_q_heads, int m, int t, int tokens_per_split, Window w = {0, 0})
 {
-    if (tokens_per_split == 0 && chunk_by_token(f, batch, n_q_heads, m, t)) {
+    if (tokens_per_split == 0 && chunk_by_token(f, batch, n_q_heads, m, chunk_span(m, t, w))) {
         size_t need = 0;
-        for (int j = 0; j < m; ++j) need = std::max(need, chunk_token_call(f, batch, n_q_heads, m, t, j).workspace);
+        for (int j = 0; j < m; ++j) need = std::max(need, chunk_token_call(f, batch, n_q_heads, m, t, j, w).workspace);
         return need;
     }
+    t = chunk_span(m, t, w);
     const int tiles = tokens_per_split ? tokens_per_split / kTileTokens : chunk_tiles_per_split(f, batch, n_q_heads, m, t);
     const int n_tiles = (t + kTileTokens - 1) / kTileTokens;
     const int n_split = (n_tiles + tiles - 1) / tiles;
@@ -848,13 +852,13 @@ size_t chunk_workspace(const Derived& f, int batch, int n_q_heads, int m, int t,
 // that leaves a quarter of the CUs or more without an item and the chunk can go token by token, it does: 5 tokens
 // of batch 4 x 131072, 32 KV heads, CQ-8c8b: 440 us token by token, about 560 in one piece (271 us with two,
 // which that workspace does not hold).
-int chunk_lds_tiles(const Derived& f, int batch, int n_q_heads, int m, int t, bool by_token)
+int chunk_lds_tiles(const Derived& f, int batch, int n_q_heads, int m, int t, bool by_token, Window w)
 {
     const ChunkLdsPlan p = chunk_lds_plan(f, n_q_heads, m);
-    const int n_tiles = (t + kTileTokens - 1) / kTileTokens;
+    const int n_tiles = (chunk_span(m, t, w) + kTileTokens - 1) / kTileTokens;
     const long base = batch;
     const size_t piece = sizeof(float) * (size_t)batch * m * n_q_heads * (f.head_dim + kPartialHeader);
-    const long fit = std::max<long>(1, (long)(chunk_workspace(f, batch, n_q_heads, m, t, 0) / piece));
+    const long fit = std::max<long>(1, (long)(chunk_workspace(f, batch, n_q_heads, m, t, 0, w) / piece));
     if (by_token && base * f.n_kv_heads * fit < 192) return 0;
     long best_ns = 1, best_cost = -1;
     for (long ns = 1; ns <= std::min<long>(fit, std::max(1, n_tiles / 8)); ++ns) {
@@ -875,7 +879,7 @@ cq_status chunk_common(const void* q, const void* k_codes, const void* v_codes,
                        int32_t batch, int32_t n_q_heads, int32_t m, int32_t t, int32_t t_cap, const cq_page_table* pages,
                        const int32_t* seq_lens, int32_t tokens_per_split,
                        void* out, void* workspace, size_t workspace_bytes, void* stream,
-                       const void* rope_table = nullptr, int32_t rope_positions = 0)
+                       const void* rope_table = nullptr, int32_t rope_positions = 0, const Window* window = nullptr)
 {
     Derived f;
     cq_status st = derive(fmt, &f);
@@ -903,19 +907,22 @@ cq_status chunk_common(const void* q, const void* k_codes, const void* v_codes,
     if (!aligned16(q) || !aligned16(k_codes) || !aligned16(v_codes) || !aligned16(k_centroids) ||
         !aligned16(v_centroids) || !aligned16(out) || !aligned16(workspace))
         return CQ_ERR_INVALID_ARG;
-    const int n_tiles = (t + kTileTokens - 1) / kTileTokens;
+    Window win = window ? *window : Window{0, 0};
+    if (window && (st = check_window(&win, t)) != CQ_OK) return st;
+    const int span = chunk_span(m, t, win);
+    const int n_tiles = (span + kTileTokens - 1) / kTileTokens;
     const size_t rows = (size_t)batch * m * n_q_heads;
-    const bool by_token = !rope && tokens_per_split == 0 && chunk_by_token(f, batch, n_q_heads, m, t);
+    const bool by_token = !rope && tokens_per_split == 0 && chunk_by_token(f, batch, n_q_heads, m, span);
     int tiles = 0;
     if (by_token) {
         for (int j = 0; j < m; ++j) {
-            const TokenCall c = chunk_token_call(f, batch, n_q_heads, m, t, j);
+            const TokenCall c = chunk_token_call(f, batch, n_q_heads, m, t, j, win);
             if (c.workspace && !workspace) return CQ_ERR_INVALID_ARG;
             if (workspace_bytes < c.workspace) return CQ_ERR_WORKSPACE_TOO_SMALL;
             if ((int64_t)batch * n_q_heads * c.n_split > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
         }
     } else {
-        tiles = tokens_per_split ? tokens_per_split / kTileTokens : chunk_tiles_per_split(f, batch, n_q_heads, m, t);
+        tiles = tokens_per_split ? tokens_per_split / kTileTokens : chunk_tiles_per_split(f, batch, n_q_heads, m, span);
         const int n_split = (n_tiles + tiles - 1) / tiles;
         if (n_split > 1) {
             if (!workspace) return CQ_ERR_INVALID_ARG;
@@ -924,12 +931,12 @@ cq_status chunk_common(const void* q, const void* k_codes, const void* v_codes,
     }
     int lds_tiles = 0;
     if (chunk_in_lds(f, n_q_heads, m, n_tiles, tokens_per_split ? std::min(tiles, n_tiles) : n_tiles, rope))
-        lds_tiles = tokens_per_split ? tiles : chunk_lds_tiles(f, batch, n_q_heads, m, t, by_token);
+        lds_tiles = tokens_per_split ? tiles : chunk_lds_tiles(f, batch, n_q_heads, m, t, by_token, win);
     if (by_token && !lds_tiles) {
         const int64_t row = (int64_t)n_q_heads * f.head_dim;
         for (int j = 0; j < m; ++j) {           // (in stream order: the calls share the workspace)
-            const TokenCall c = chunk_token_call(f, batch, n_q_heads, m, t, j);
-            DecodeArgs a;
+            const TokenCall c = chunk_token_call(f, batch, n_q_heads, m, t, j, win);
+            DecodeViewArgs a;
             a.layers = nullptr;
             a.n_layers = 1;
             a.wgs_per_layer = batch * n_q_heads * c.n_split;
@@ -955,7 +962,11 @@ cq_status chunk_common(const void* q, const void* k_codes, const void* v_codes,
             a.split_given = false;
             a.partials = static_cast<float*>(workspace);
             a.f = f;
-            if ((st = launch_decode(a, static_cast<hipStream_t>(stream))) != CQ_OK) return st;
+            a.window = win.window;
+            a.n_sink = win.n_sink;
+            a.scores = nullptr;
+            st = window ? launch_decode_view(a, static_cast<hipStream_t>(stream)) : launch_decode(a, static_cast<hipStream_t>(stream));
+            if (st != CQ_OK) return st;
         }
         return CQ_OK;
     }
@@ -966,7 +977,7 @@ cq_status chunk_common(const void* q, const void* k_codes, const void* v_codes,
     const int64_t row_blocks = ((int64_t)m * qper + rpw - 1) / rpw;
     if ((int64_t)batch * f.n_kv_heads * row_blocks * n_split > 0x7fffffffLL || rows * n_split > 0x7fffffffULL)
         return CQ_ERR_INVALID_ARG;
-    ChunkArgs a;
+    ChunkViewArgs a;
     a.q = static_cast<const uint16_t*>(q);
     a.k_codes = static_cast<const uint8_t*>(k_codes);
     a.v_codes = static_cast<const uint8_t*>(v_codes);
@@ -986,8 +997,11 @@ cq_status chunk_common(const void* q, const void* k_codes, const void* v_codes,
     a.rope_tile_tab = static_cast<const float2*>(rope_table);
     a.rope_lane_tab = rope ? a.rope_tile_tab + (size_t)(rope_positions / kTileTokens) * 64 : nullptr;
     a.f = f;
-    if (!lds_tiles) return launch_chunk_attention(a, static_cast<hipStream_t>(stream));
-    if ((st = launch_chunk_lds(a, static_cast<hipStream_t>(stream))) != CQ_OK || n_split == 1) return st;
+    a.window = win.window;
+    a.n_sink = win.n_sink;
+    if (!lds_tiles) return window ? launch_chunk_attention_window(a, static_cast<hipStream_t>(stream)) : launch_chunk_attention(a, static_cast<hipStream_t>(stream));
+    st = window ? launch_chunk_lds_window(a, static_cast<hipStream_t>(stream)) : launch_chunk_lds(a, static_cast<hipStream_t>(stream));
+    if (st != CQ_OK || n_split == 1) return st;
     return launch_decode_merge(a.partials, a.out, batch * m * n_q_heads, n_q_heads, (int64_t)n_q_heads * f.head_dim, n_split, f.head_dim,
                                static_cast<hipStream_t>(stream));
 }
@@ -1032,6 +1046,40 @@ cq_status cq_chunk_attention_paged(const void* q, const void* k_pool, const void
     if (!pages) return CQ_ERR_INVALID_ARG;
     return chunk_common(q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, batch, n_q_heads, m, t, 0, pages,
                         seq_lens, tokens_per_split, out, workspace, workspace_bytes, stream);
+}
+
+size_t cq_chunk_window_workspace_bytes(const cq_format* fmt, int32_t batch, int32_t n_q_heads, int32_t m, int32_t t,
+                                       int32_t window, int32_t n_sink, int32_t tokens_per_split)
+{
+    Derived f;
+    Window w{window, n_sink};
+    if (derive(fmt, &f) != CQ_OK || f.head_dim != 128) return 0;
+    if (batch <= 0 || n_q_heads <= 0 || n_q_heads % f.n_kv_heads != 0 || m <= 0 || t < m || check_window(&w, t) != CQ_OK) return 0;
+    if (tokens_per_split < 0 || tokens_per_split % kTileTokens != 0) return 0;
+    return chunk_workspace(f, batch, n_q_heads, m, t, tokens_per_split, w);
+}
+
+cq_status cq_chunk_attention_window(const void* q, const void* k_codes, const void* v_codes,
+                                    const void* k_centroids, const void* v_centroids, float scale, const cq_format* fmt,
+                                    int32_t batch, int32_t n_q_heads, int32_t m, int32_t t, int32_t t_cap,
+                                    const int32_t* seq_lens, int32_t window, int32_t n_sink, int32_t tokens_per_split,
+                                    void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const Window w{window, n_sink};
+    return chunk_common(q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, batch, n_q_heads, m, t, t_cap, nullptr,
+                        seq_lens, tokens_per_split, out, workspace, workspace_bytes, stream, nullptr, 0, &w);
+}
+
+cq_status cq_chunk_attention_window_paged(const void* q, const void* k_pool, const void* v_pool,
+                                          const void* k_centroids, const void* v_centroids, float scale, const cq_format* fmt,
+                                          int32_t batch, int32_t n_q_heads, int32_t m, int32_t t, const cq_page_table* pages,
+                                          const int32_t* seq_lens, int32_t window, int32_t n_sink, int32_t tokens_per_split,
+                                          void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!pages) return CQ_ERR_INVALID_ARG;
+    const Window w{window, n_sink};
+    return chunk_common(q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, batch, n_q_heads, m, t, 0, pages,
+                        seq_lens, tokens_per_split, out, workspace, workspace_bytes, stream, nullptr, 0, &w);
 }
 
 size_t cq_layer_table_bytes(int32_t n_layers)

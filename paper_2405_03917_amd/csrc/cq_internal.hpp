@@ -173,8 +173,13 @@ struct ChunkArgs {
     const float2* rope_lane_tab;
     Derived f;
 };
+// ... each through its own sliding window, with sinks.
+struct ChunkViewArgs : ChunkArgs {
+    int window, n_sink;
+};
 int chunk_rows_per_workgroup(int rows_per_kv_head);
 cq_status launch_chunk_attention(const ChunkArgs& a, hipStream_t stream);
+cq_status launch_chunk_attention_window(const ChunkViewArgs& a, hipStream_t stream);
 // Few rows per KV head, codebooks in LDS (cq_chunk_lds.hip: CQ-8c8b and CQ-4c8b).
 constexpr int kChunkLdsRows = 64;
 struct ChunkLdsPlan {
@@ -183,6 +188,7 @@ struct ChunkLdsPlan {
 };
 ChunkLdsPlan chunk_lds_plan(const Derived& f, int n_q_heads, int m);
 cq_status launch_chunk_lds(const ChunkArgs& a, hipStream_t stream);
+cq_status launch_chunk_lds_window(const ChunkViewArgs& a, hipStream_t stream);
 
 // Largest tokens_per_split the decode kernel's on-chip score buffer can hold.
 int decode_max_tiles_per_split(const Derived& f);

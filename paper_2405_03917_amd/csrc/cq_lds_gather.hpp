@@ -95,6 +95,27 @@ __device__ __forceinline__ unsigned entry(unsigned z, int k, unsigned base)
     return __builtin_amdgcn_udot4(z, (2u * C) << (8 * k), base, false);
 }
 
+// The tiles that the rows at positions first .. last see through their windows, numbered without gaps: the sinks' tiles in
+// front of the earliest window (`head` of them), then from its first tile on, `skip` further on in the cache.
+struct ChunkSeen {
+    int n_tiles, head, skip;
+    __device__ __forceinline__ ChunkSeen() = default;
+    __device__ __forceinline__ ChunkSeen(const ChunkViewArgs& a, int first, int last)
+    {
+        const int at = max(0, first - a.window + 1) / kTileTokens;
+        head = min((a.n_sink + kTileTokens - 1) / kTileTokens, at);
+        skip = at - head;
+        n_tiles = last / kTileTokens + 1 - skip;
+    }
+    __device__ __forceinline__ int tile(int i) const { return i < head ? i : i + skip; }
+};
+// whether some row at a position up to `last` does not see the start of tile `tile` for its window
+__device__ __forceinline__ bool before_window(const ChunkViewArgs& a, int tile, int last)
+{
+    return tile * kTileTokens <= last - a.window && tile * kTileTokens + kTileTokens > a.n_sink;
+}
+__device__ __forceinline__ bool in_window(const ChunkViewArgs& a, int tok, int pos) { return tok <= pos && (tok > pos - a.window || tok < a.n_sink); }
+
 template <int ABID>
 __device__ __forceinline__ float4_t mfma_heads(half4_t q, half4_t k, float4_t c)
 {
