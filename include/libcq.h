@@ -604,6 +604,50 @@ CQ_API cq_status cq_decode_attention_weights_paged(const void *q, const void *k_
                                             void *out, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Eviction.  cq_select_tokens names the tokens that stay, per sequence and KV head; cq_compact_cache[_paged] moves them to
+ * the front of their cache, or of another one.
+ *
+ * cq_select_tokens   of the first t_n = seq_lens[n] (default t) tokens of stream (n, h): all, if there are no more than
+ * `keep`; else its first n_sink, its last n_recent, and those of largest weight between them, `keep` in all.  Equal weights:
+ * the lowest positions stay; both zeros are equal; a weight that is no number ranks below every number.
+ *   weights           device, fp32 [batch][n_kv_heads][weights_stride], weights_stride >= t (cq_decode_attention_weights, ...)
+ *   seq_lens          device int32 [batch] or NULL; values are clamped into [0, t]
+ *   keep              >= 1; n_sink, n_recent >= 0, n_sink + n_recent <= keep
+ *   kept              out, device int32 [batch][n_kv_heads][keep]: positions in ascending order, -1 behind the last
+ *   kept_lens         out, device int32 [batch]: min(t_n, keep), the sequence's length from then on (all its KV heads
+ *                     keep as many tokens, each its own)
+ * One kernel; the result is a function of the weights alone.
+ *
+ * cq_compact_cache   position r of stream (n, h) receives the codes (and, unless both are NULL, the accumulator) of
+ * position kept[n][h][r], for r < kept_lens[n].  Accumulators of positions kept_lens[n] .. min(t, t_cap_out) - 1 become
+ * zero, as those of tokens appended next have to be; codes behind kept_lens[n] are left as they are.
+ *   k_out, v_out, weights_out   the inputs themselves (in place; t_cap_out = t_cap, weights_out_stride = weights_stride), or
+ *                     buffers apart from all others; their old contents behind what is written stay.  keep <= t_cap_out;
+ *                     weights_out_stride >= keep and >= min(t, t_cap_out)
+ *   kept, kept_lens   device, as written by cq_select_tokens; values outside [0, t) and [0, keep] are clamped
+ *   workspace         device, cq_compact_workspace_bytes(...) bytes; may be NULL where no output is an input
+ *   Any format, sub-byte ones included.  Keys stay as they are stored: those rotated to their positions keep them, those
+ *   cached before the rotary embedding take the positions they move to.
+ * cq_compact_cache_paged   the same from the pages of one block table to those of another (the same, or another one over
+ * the same pools, or over other pools).  Where pools are the same, everything is read before anything is written.  Two
+ * sequences must not share pages that are written.
+ * Errors: CQ_ERR_INVALID_ARG (null, misaligned or overlapping pointers, sizes out of range, more than 65535 streams),
+ * CQ_ERR_UNSUPPORTED (format), CQ_ERR_WORKSPACE_TOO_SMALL, CQ_ERR_HIP.
+ */
+CQ_API cq_status cq_select_tokens(const float *weights, int64_t weights_stride, int32_t batch, int32_t n_kv_heads, int32_t t,
+                           const int32_t *seq_lens, int32_t keep, int32_t n_sink, int32_t n_recent,
+                           int32_t *kept, int32_t *kept_lens, void *stream);
+CQ_API size_t cq_compact_workspace_bytes(const cq_format *fmt, int32_t batch, int32_t keep);
+CQ_API cq_status cq_compact_cache(const void *k_codes, const void *v_codes, const float *weights, int64_t weights_stride, const cq_format *fmt,
+                           int32_t batch, int32_t t, int32_t t_cap, const int32_t *kept, const int32_t *kept_lens, int32_t keep,
+                           void *k_out, void *v_out, float *weights_out, int64_t weights_out_stride, int32_t t_cap_out,
+                           void *workspace, size_t workspace_bytes, void *stream);
+CQ_API cq_status cq_compact_cache_paged(const void *k_pool, const void *v_pool, const float *weights, int64_t weights_stride, const cq_format *fmt,
+                                 int32_t batch, int32_t t, const cq_page_table *pages, const int32_t *kept, const int32_t *kept_lens, int32_t keep,
+                                 void *k_pool_out, void *v_pool_out, float *weights_out, int64_t weights_out_stride, const cq_page_table *pages_out,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * cq_dequantize -- the inverse lookup ("dequantization", Section 2.2; CQ(A) of Eq. 5 as values):
  * out[n][t][g c + i] = centroids[g][code(n, t_offset + t, g)][i] for t = 0 .. t_count - 1, bit
  * for bit the stored fp16 centroids.  For callers that need dense keys / values (e.g. a

@@ -38,6 +38,7 @@ EXPORTS = (
     "cq_decode_attention_window_paged", "cq_decode_step_window", "cq_decode_step_window_paged",
     "cq_chunk_window_workspace_bytes", "cq_chunk_attention_window", "cq_chunk_attention_window_paged",
     "cq_decode_weights_workspace_bytes", "cq_decode_attention_weights", "cq_decode_attention_weights_paged",
+    "cq_select_tokens", "cq_compact_workspace_bytes", "cq_compact_cache", "cq_compact_cache_paged",
     "cq_probe_stream_read", "cq_probe_copy", "cq_probe_mfma", "cq_probe_decode_plan",
 )
 
@@ -214,6 +215,13 @@ def load() -> ctypes.CDLL:
     for at, name in ((i32, "cq_decode_attention_weights"), (pp, "cq_decode_attention_weights_paged")):
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = [vp, vp, vp, vp, vp, f32, fp, i32, i32, i32, at, vp, i32, vp, i64, f32, vp, vp, size, vp]
+    lib.cq_select_tokens.restype = ctypes.c_int
+    lib.cq_select_tokens.argtypes = [vp, i64, i32, i32, i32, vp, i32, i32, i32, vp, vp, vp]
+    lib.cq_compact_workspace_bytes.restype = size
+    lib.cq_compact_workspace_bytes.argtypes = [fp, i32, i32]
+    for at, name in ((i32, "cq_compact_cache"), (pp, "cq_compact_cache_paged")):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = [vp, vp, vp, i64, fp, i32, i32, at, vp, vp, i32, vp, vp, vp, i64, at, vp, size, vp]
     lib.cq_probe_copy.restype = ctypes.c_int
     lib.cq_probe_copy.argtypes = [vp, vp, ctypes.c_size_t, vp]
     lib.cq_probe_mfma.restype = ctypes.c_int
@@ -1328,3 +1336,96 @@ def cq_decode_attention_weights_paged(q, k_pool, v_pool, k_centroids, v_centroid
                                                  pages, seq_lens, tokens_per_split, out, workspace)
     call(stream)
     return out
+
+
+def prepare_select_tokens(weights, t: int, keep: int, n_sink: int = 0, n_recent: int = 0, seq_lens=None, kept=None, kept_lens=None):
+    """Check and marshal the arguments of cq_select_tokens once.  Returns (call, kept, kept_lens)."""
+    import torch
+    _dev(weights, torch.float32, "weights")
+    if weights.dim() != 3 or not weights.is_contiguous() or weights.shape[2] < t:
+        raise ValueError("weights must be contiguous fp32 [B, n_kv_heads, tokens >= t]")
+    batch, hkv, stride = (int(x) for x in weights.shape)
+    sl = _check_seq_lens(seq_lens, batch)
+    if keep < 1:
+        raise ValueError("keep must be positive")
+    if kept is None:
+        kept = torch.empty((batch, hkv, keep), dtype=torch.int32, device=weights.device)
+    if kept_lens is None:
+        kept_lens = torch.empty((batch,), dtype=torch.int32, device=weights.device)
+    for what, x, shape in (("kept", kept, (batch, hkv, keep)), ("kept_lens", kept_lens, (batch,))):
+        _dev(x, torch.int32, what)
+        if tuple(x.shape) != shape or not x.is_contiguous():
+            raise ValueError(f"{what} must be contiguous int32 {list(shape)}")
+    _same_device(weights, seq_lens, kept, kept_lens)
+    args = (weights.data_ptr(), stride, batch, hkv, t, sl, keep, n_sink, n_recent, kept.data_ptr(), kept_lens.data_ptr())
+    return PreparedCall(load().cq_select_tokens, args, (weights, seq_lens, kept, kept_lens), "cq_select_tokens"), kept, kept_lens
+
+
+def cq_select_tokens(weights, t: int, keep: int, n_sink: int = 0, n_recent: int = 0, seq_lens=None, kept=None, kept_lens=None, stream=None):
+    """The `keep` tokens that stay of every sequence and KV head: its first n_sink, its last n_recent, and the heaviest by
+    `weights` fp32 [B, n_kv_heads, tokens].  Returns (kept int32 [B, n_kv_heads, keep], ascending, -1 behind the last; kept_lens
+    int32 [B], the sequences' new lengths)."""
+    call, kept, kept_lens = prepare_select_tokens(weights, t, keep, n_sink, n_recent, seq_lens, kept, kept_lens)
+    call(stream)
+    return kept, kept_lens
+
+
+def cq_compact_workspace_bytes(fmt: CQFormat, batch: int, keep: int) -> int:
+    return int(load().cq_compact_workspace_bytes(ctypes.byref(fmt._c()), batch, keep))
+
+
+def prepare_compact_cache(k_codes, v_codes, weights, fmt: CQFormat, kept, kept_lens, t: int, t_cap: int, k_out=None, v_out=None,
+                          weights_out=None, t_cap_out=None, pages=None, pages_out=None, workspace=None) -> PreparedCall:
+    """Check and marshal the arguments of cq_compact_cache (with `pages`, of its paged form) once.  Outputs that are not given
+    are the inputs: in place."""
+    import torch
+    k_out, v_out = (k_codes if k_out is None else k_out), (v_codes if v_out is None else v_out)
+    weights_out = weights if weights_out is None else weights_out
+    t_cap_out = t_cap if t_cap_out is None else t_cap_out
+    pages_out = pages if pages_out is None else pages_out
+    if (pages is None) != (pages_out is None):
+        raise ValueError("pages_out goes with pages")
+    _dev(kept, torch.int32, "kept")
+    _dev(kept_lens, torch.int32, "kept_lens")
+    if kept.dim() != 3 or kept.shape[1] != fmt.n_kv_heads or not kept.is_contiguous():
+        raise ValueError("kept must be contiguous int32 [B, n_kv_heads, keep]")
+    batch, keep = int(kept.shape[0]), int(kept.shape[2])
+    if tuple(kept_lens.shape) != (batch,) or not kept_lens.is_contiguous():
+        raise ValueError("kept_lens must be contiguous int32 [B]")
+    _check_caches(fmt, batch, t_cap, pages, k_codes, v_codes)
+    _check_caches(fmt, batch, t_cap_out, pages_out, k_out, v_out)
+    stride = stride_out = 0
+    if weights is not None:
+        stride = _check_weights(weights, batch, fmt, t)
+        stride_out = _check_weights(weights_out, batch, fmt, max(keep, min(t, t_cap_out if pages_out is None else 64 * pages_out.max_tiles)), "weights_out")
+    elif weights_out is not None:
+        raise ValueError("weights_out goes with weights")
+    if k_out is k_codes or v_out is v_codes or (weights is not None and weights_out is weights) or workspace is not None \
+            or k_out.data_ptr() == k_codes.data_ptr() or v_out.data_ptr() == v_codes.data_ptr():
+        workspace = _workspace(workspace, cq_compact_workspace_bytes(fmt, batch, keep), kept.device, "cq_compact_workspace_bytes")
+    _same_device(k_codes, v_codes, weights, kept, kept_lens, k_out, v_out, weights_out, workspace,
+                 None if pages is None else pages.block_table, None if pages_out is None else pages_out.block_table)
+    f = fmt._c()
+    ptr = lambda x: None if x is None else x.data_ptr()  # noqa: E731
+    args = (k_codes.data_ptr(), v_codes.data_ptr(), ptr(weights), stride, ctypes.byref(f), batch, t,
+            t_cap if pages is None else ctypes.byref(pages._c), kept.data_ptr(), kept_lens.data_ptr(), keep, k_out.data_ptr(), v_out.data_ptr(),
+            ptr(weights_out), stride_out, t_cap_out if pages is None else ctypes.byref(pages_out._c), ptr(workspace),
+            0 if workspace is None else workspace.numel())
+    name = "cq_compact_cache" + ("" if pages is None else "_paged")
+    keep_alive = (k_codes, v_codes, weights, kept, kept_lens, k_out, v_out, weights_out, workspace, f, pages, pages_out)
+    return PreparedCall(getattr(load(), name), args, keep_alive, name)
+
+
+def cq_compact_cache(k_codes, v_codes, weights, fmt: CQFormat, kept, kept_lens, t: int, t_cap: int, k_out=None, v_out=None,
+                     weights_out=None, t_cap_out=None, workspace=None, stream=None) -> None:
+    """Move the tokens `kept` (cq_select_tokens) of every sequence and KV head, codes and accumulators (weights None: codes
+    alone), to positions 0, 1, ...: in place, or into k_out, v_out, weights_out of capacity t_cap_out."""
+    prepare_compact_cache(k_codes, v_codes, weights, fmt, kept, kept_lens, t, t_cap, k_out, v_out, weights_out, t_cap_out,
+                          workspace=workspace)(stream)
+
+
+def cq_compact_cache_paged(k_pool, v_pool, weights, fmt: CQFormat, kept, kept_lens, t: int, pages: PageTable, k_pool_out=None,
+                           v_pool_out=None, weights_out=None, pages_out=None, workspace=None, stream=None) -> None:
+    """cq_compact_cache from the pages of `pages` to those of `pages_out` (default: in place)."""
+    prepare_compact_cache(k_pool, v_pool, weights, fmt, kept, kept_lens, t, 0, k_pool_out, v_pool_out, weights_out, 0, pages, pages_out,
+                          workspace)(stream)

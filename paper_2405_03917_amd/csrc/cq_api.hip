@@ -1082,6 +1082,126 @@ cq_status cq_chunk_attention_window_paged(const void* q, const void* k_pool, con
                         seq_lens, tokens_per_split, out, workspace, workspace_bytes, stream, nullptr, 0, &w);
 }
 
+cq_status cq_select_tokens(const float* weights, int64_t weights_stride, int32_t batch, int32_t n_kv_heads, int32_t t,
+                           const int32_t* seq_lens, int32_t keep, int32_t n_sink, int32_t n_recent,
+                           int32_t* kept, int32_t* kept_lens, void* stream)
+{
+    if (!weights || !kept || !kept_lens || !aligned16(weights) || !aligned16(kept) || !aligned16(kept_lens)) return CQ_ERR_INVALID_ARG;
+    if (batch <= 0 || n_kv_heads <= 0 || t <= 0 || weights_stride < t || keep <= 0) return CQ_ERR_INVALID_ARG;
+    if (n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > keep) return CQ_ERR_INVALID_ARG;
+    if ((int64_t)batch * n_kv_heads > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
+    const SelectArgs a{weights, weights_stride, seq_lens, batch, n_kv_heads, t, keep, n_sink, n_recent, kept, kept_lens};
+    return launch_select_tokens(a, static_cast<hipStream_t>(stream));
+}
+
+namespace {
+
+size_t compact_codes_bytes(const Derived& f, int32_t batch, int32_t keep)
+{
+    return (size_t)2 * batch * f.n_kv_heads * ((keep + (size_t)kTileTokens - 1) / kTileTokens) * f.tile_bytes;
+}
+
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + b_bytes && y < x + a_bytes;
+}
+
+cq_status compact_common(const void* k_codes, const void* v_codes, const float* weights, int64_t weights_stride, const cq_format* fmt,
+                         int32_t batch, int32_t t, int32_t t_cap, const cq_page_table* pages, const int32_t* kept, const int32_t* kept_lens,
+                         int32_t keep, void* k_out, void* v_out, float* weights_out, int64_t weights_out_stride, int32_t t_cap_out,
+                         const cq_page_table* pages_out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    Derived f;
+    cq_status st = derive_any(fmt, &f);
+    if (st != CQ_OK) return st;
+    CompactArgs a;
+    size_t in_bytes, out_bytes;
+    if (pages) {
+        if ((st = paged_map(f, pages, batch, &a.map_in, &t_cap)) != CQ_OK || (st = paged_map(f, pages_out, batch, &a.map_out, &t_cap_out)) != CQ_OK) return st;
+        in_bytes = (size_t)pages->n_pages * f.n_kv_heads * f.tile_bytes;
+        out_bytes = (size_t)pages_out->n_pages * f.n_kv_heads * f.tile_bytes;
+    } else {
+        if (t_cap <= 0 || t_cap % kTileTokens != 0 || t_cap_out <= 0 || t_cap_out % kTileTokens != 0) return CQ_ERR_INVALID_ARG;
+        a.map_in = contiguous_map(f, t_cap);
+        a.map_out = contiguous_map(f, t_cap_out);
+        in_bytes = cq_cache_bytes(fmt, batch, t_cap);
+        out_bytes = cq_cache_bytes(fmt, batch, t_cap_out);
+    }
+    if (!k_codes || !v_codes || !k_out || !v_out || !kept || !kept_lens || (weights == nullptr) != (weights_out == nullptr)) return CQ_ERR_INVALID_ARG;
+    if (batch <= 0 || t <= 0 || t > t_cap || keep <= 0 || keep > t_cap_out) return CQ_ERR_INVALID_ARG;
+    if ((int64_t)batch * f.n_kv_heads > 65535) return CQ_ERR_INVALID_ARG;
+    if (!aligned16(k_codes) || !aligned16(v_codes) || !aligned16(k_out) || !aligned16(v_out) || !aligned16(kept) || !aligned16(kept_lens) ||
+        !aligned16(weights) || !aligned16(weights_out) || !aligned16(workspace))
+        return CQ_ERR_INVALID_ARG;
+    const int32_t end = std::min(t, t_cap_out);
+    if (weights && (weights_stride < t || weights_out_stride < end || weights_out_stride < keep)) return CQ_ERR_INVALID_ARG;
+    // Each output is either its own input, moved in place, or apart from everything else.
+    const bool same_k = k_out == k_codes, same_v = v_out == v_codes, same_w = weights && weights_out == weights;
+    const size_t streams = (size_t)batch * f.n_kv_heads;
+    const size_t w_bytes = weights ? sizeof(float) * ((streams - 1) * weights_stride + t) : 0;
+    const size_t wo_bytes = weights ? sizeof(float) * ((streams - 1) * weights_out_stride + std::max(end, keep)) : 0;
+    if (overlap(k_codes, in_bytes, v_codes, in_bytes) || overlap(k_out, out_bytes, v_out, out_bytes)) return CQ_ERR_INVALID_ARG;
+    if (overlap(k_out, out_bytes, v_codes, in_bytes) || overlap(v_out, out_bytes, k_codes, in_bytes)) return CQ_ERR_INVALID_ARG;
+    if ((!same_k && overlap(k_out, out_bytes, k_codes, in_bytes)) || (!same_v && overlap(v_out, out_bytes, v_codes, in_bytes))) return CQ_ERR_INVALID_ARG;
+    if (!pages && (same_k || same_v) && t_cap_out != t_cap) return CQ_ERR_INVALID_ARG;
+    if (weights && (same_w ? weights_out_stride != weights_stride : overlap(weights_out, wo_bytes, weights, w_bytes))) return CQ_ERR_INVALID_ARG;
+    const bool in_place = same_k || same_v || same_w;
+    const size_t codes = round256(compact_codes_bytes(f, batch, keep));
+    a.work = nullptr;
+    a.work_weights = nullptr;
+    if (in_place) {
+        if (!workspace) return CQ_ERR_INVALID_ARG;
+        if (workspace_bytes < codes + sizeof(float) * streams * keep) return CQ_ERR_WORKSPACE_TOO_SMALL;
+        a.work = static_cast<uint8_t*>(workspace);
+        a.work_weights = reinterpret_cast<float*>(a.work + codes);
+    }
+    a.in[0] = static_cast<const uint8_t*>(k_codes);
+    a.in[1] = static_cast<const uint8_t*>(v_codes);
+    a.out[0] = static_cast<uint8_t*>(k_out);
+    a.out[1] = static_cast<uint8_t*>(v_out);
+    a.weights = weights;
+    a.weights_stride = weights_stride;
+    a.weights_out = weights_out;
+    a.weights_out_stride = weights_out_stride;
+    a.kept = kept;
+    a.kept_lens = kept_lens;
+    a.batch = batch;
+    a.n_kv_heads = f.n_kv_heads;
+    a.t = t;
+    a.keep = keep;
+    a.t_cap_out = t_cap_out;
+    return launch_compact(a, f, static_cast<hipStream_t>(stream));
+}
+
+}  // namespace
+
+size_t cq_compact_workspace_bytes(const cq_format* fmt, int32_t batch, int32_t keep)
+{
+    Derived f;
+    if (derive_any(fmt, &f) != CQ_OK || batch <= 0 || keep <= 0) return 0;
+    return round256(compact_codes_bytes(f, batch, keep)) + sizeof(float) * (size_t)batch * f.n_kv_heads * keep;
+}
+
+cq_status cq_compact_cache(const void* k_codes, const void* v_codes, const float* weights, int64_t weights_stride, const cq_format* fmt,
+                           int32_t batch, int32_t t, int32_t t_cap, const int32_t* kept, const int32_t* kept_lens, int32_t keep,
+                           void* k_out, void* v_out, float* weights_out, int64_t weights_out_stride, int32_t t_cap_out,
+                           void* workspace, size_t workspace_bytes, void* stream)
+{
+    return compact_common(k_codes, v_codes, weights, weights_stride, fmt, batch, t, t_cap, nullptr, kept, kept_lens, keep, k_out, v_out,
+                          weights_out, weights_out_stride, t_cap_out, nullptr, workspace, workspace_bytes, stream);
+}
+
+cq_status cq_compact_cache_paged(const void* k_pool, const void* v_pool, const float* weights, int64_t weights_stride, const cq_format* fmt,
+                                 int32_t batch, int32_t t, const cq_page_table* pages, const int32_t* kept, const int32_t* kept_lens, int32_t keep,
+                                 void* k_pool_out, void* v_pool_out, float* weights_out, int64_t weights_out_stride, const cq_page_table* pages_out,
+                                 void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!pages || !pages_out) return CQ_ERR_INVALID_ARG;
+    return compact_common(k_pool, v_pool, weights, weights_stride, fmt, batch, t, 0, pages, kept, kept_lens, keep, k_pool_out, v_pool_out,
+                          weights_out, weights_out_stride, 0, pages_out, workspace, workspace_bytes, stream);
+}
+
 size_t cq_layer_table_bytes(int32_t n_layers)
 {
     return n_layers > 0 ? sizeof(LayerPtrs) * (size_t)n_layers : 0;

@@ -204,6 +204,34 @@ struct DequantArgs {
 };
 cq_status launch_dequantize(const DequantArgs& a, hipStream_t stream);
 
+// Eviction (cq_evict.hip): the tokens that stay, per (sequence, KV head) stream, and their move.
+struct SelectArgs {
+    const float* weights;     // [stream][weights_stride]
+    int64_t weights_stride;
+    const int32_t* seq_lens;
+    int batch, n_kv_heads, t, keep, n_sink, n_recent;
+    int32_t* kept;            // [stream][keep]: ascending positions, -1 behind the last
+    int32_t* kept_lens;       // [sequence]
+};
+cq_status launch_select_tokens(const SelectArgs& a, hipStream_t stream);
+
+struct CompactArgs {
+    const uint8_t* in[2];     // key and value caches (or pools)
+    uint8_t* out[2];
+    CacheMap map_in, map_out;
+    const float* weights;     // null: no accumulators to move
+    int64_t weights_stride;
+    float* weights_out;
+    int64_t weights_out_stride;
+    const int32_t* kept;
+    const int32_t* kept_lens;
+    int batch, n_kv_heads, t, keep, t_cap_out;
+    // what is read may be written (null: it is not): the tokens go here first, tile by tile as the caches hold them
+    uint8_t* work;
+    float* work_weights;
+};
+cq_status launch_compact(const CompactArgs& a, const Derived& f, hipStream_t stream);
+
 // Centroid learning: k-means++ (do_init) or given starting centroids, then n_iter Lloyd iterations.
 struct KMeansArgs {
     const uint16_t* x;        // fp16 [n][D]
