@@ -604,6 +604,29 @@ CQ_API cq_status cq_decode_attention_weights_paged(const void *q, const void *k_
                                             void *out, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * cq_chunk_weights[_paged] -- the attention weights of the LAST m tokens of each sequence, added up: for every token i < t_n,
+ *     weights[n][h][i] = decay * weights[n][h][i] + sum over j < m and the query heads of h of softmax_j(scale q_j.k)_i
+ * with query token j at position t_n - m + j, attending to tokens 0 .. t_n - m + j (a later one gets nothing from it).  For
+ * an eviction after a prompt: the last few tens of its tokens look back, or every chunk adds its weights.  Keys as
+ * stored; no values are read and no output is formed (cq_chunk_attention does that).
+ *   q                 device, fp16 [batch][m][n_q_heads][head_dim]
+ *   m                 1 <= m <= seq_lens[n] <= t <= t_cap
+ *   weights, weights_stride, decay   as in cq_decode_attention_weights
+ *   workspace         device, cq_chunk_weights_workspace_bytes(...) bytes
+ *   everything else as in cq_chunk_attention.
+ * Scores are exact products of fp16 numbers summed in fp32 on the matrix cores, computed twice: for the rows' maxima and
+ * sums, then for the weights; all in fp32, in a fixed order (no atomics): equal calls give equal bits.
+ * Errors: as cq_chunk_attention and, for the accumulators, cq_decode_attention_weights.
+ */
+CQ_API size_t cq_chunk_weights_workspace_bytes(const cq_format *fmt, int32_t batch, int32_t n_q_heads, int32_t m, int32_t t);
+CQ_API cq_status cq_chunk_weights(const void *q, const void *k_codes, const void *k_centroids, float scale, const cq_format *fmt,
+                           int32_t batch, int32_t n_q_heads, int32_t m, int32_t t, int32_t t_cap, const int32_t *seq_lens,
+                           float *weights, int64_t weights_stride, float decay, void *workspace, size_t workspace_bytes, void *stream);
+CQ_API cq_status cq_chunk_weights_paged(const void *q, const void *k_pool, const void *k_centroids, float scale, const cq_format *fmt,
+                                 int32_t batch, int32_t n_q_heads, int32_t m, int32_t t, const cq_page_table *pages, const int32_t *seq_lens,
+                                 float *weights, int64_t weights_stride, float decay, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Eviction.  cq_select_tokens names the tokens that stay, per sequence and KV head; cq_compact_cache[_paged] moves them to
  * the front of their cache, or of another one.
  *

@@ -38,6 +38,7 @@ EXPORTS = (
     "cq_decode_attention_window_paged", "cq_decode_step_window", "cq_decode_step_window_paged",
     "cq_chunk_window_workspace_bytes", "cq_chunk_attention_window", "cq_chunk_attention_window_paged",
     "cq_decode_weights_workspace_bytes", "cq_decode_attention_weights", "cq_decode_attention_weights_paged",
+    "cq_chunk_weights_workspace_bytes", "cq_chunk_weights", "cq_chunk_weights_paged",
     "cq_select_tokens", "cq_compact_workspace_bytes", "cq_compact_cache", "cq_compact_cache_paged",
     "cq_probe_stream_read", "cq_probe_copy", "cq_probe_mfma", "cq_probe_decode_plan",
 )
@@ -215,6 +216,11 @@ def load() -> ctypes.CDLL:
     for at, name in ((i32, "cq_decode_attention_weights"), (pp, "cq_decode_attention_weights_paged")):
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = [vp, vp, vp, vp, vp, f32, fp, i32, i32, i32, at, vp, i32, vp, i64, f32, vp, vp, size, vp]
+    lib.cq_chunk_weights_workspace_bytes.restype = size
+    lib.cq_chunk_weights_workspace_bytes.argtypes = [fp, i32, i32, i32, i32]
+    for at, name in ((i32, "cq_chunk_weights"), (pp, "cq_chunk_weights_paged")):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = [vp, vp, vp, f32, fp, i32, i32, i32, i32, at, vp, vp, i64, f32, vp, size, vp]
     lib.cq_select_tokens.restype = ctypes.c_int
     lib.cq_select_tokens.argtypes = [vp, i64, i32, i32, i32, vp, i32, i32, i32, vp, vp, vp]
     lib.cq_compact_workspace_bytes.restype = size
@@ -1336,6 +1342,45 @@ def cq_decode_attention_weights_paged(q, k_pool, v_pool, k_centroids, v_centroid
                                                  pages, seq_lens, tokens_per_split, out, workspace)
     call(stream)
     return out
+
+
+def cq_chunk_weights_workspace_bytes(fmt: CQFormat, batch: int, n_q_heads: int, m: int, t: int) -> int:
+    return int(load().cq_chunk_weights_workspace_bytes(ctypes.byref(fmt._c()), batch, n_q_heads, m, t))
+
+
+def prepare_chunk_weights(q, k_codes, k_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int, weights, decay: float = 1.0,
+                          pages=None, seq_lens=None, workspace=None) -> PreparedCall:
+    """Check and marshal the arguments of cq_chunk_weights (with `pages`, of its paged form) once."""
+    import torch
+    _dev(q, torch.float16, "q")
+    if q.dim() != 4 or not q.is_contiguous() or q.shape[3] != fmt.head_dim:
+        raise ValueError("q must be contiguous [B, m, Hq, head_dim]")
+    batch, m, n_q_heads = int(q.shape[0]), int(q.shape[1]), int(q.shape[2])
+    _check_centroids(fmt, k_centroids, k_centroids)
+    _check_caches(fmt, batch, t_cap, pages, k_codes)
+    sl = _check_seq_lens(seq_lens, batch)
+    stride = _check_weights(weights, batch, fmt, t)
+    workspace = _workspace(workspace, cq_chunk_weights_workspace_bytes(fmt, batch, n_q_heads, m, t), q.device, "cq_chunk_weights_workspace_bytes")
+    _same_device(q, k_codes, k_centroids, seq_lens, weights, workspace, None if pages is None else pages.block_table)
+    f = fmt._c()
+    args = (q.data_ptr(), k_codes.data_ptr(), k_centroids.data_ptr(), float(scale), ctypes.byref(f), batch, n_q_heads, m, t,
+            t_cap if pages is None else ctypes.byref(pages._c), sl, weights.data_ptr(), stride, float(decay), workspace.data_ptr(),
+            workspace.numel())
+    name = "cq_chunk_weights" + ("" if pages is None else "_paged")
+    return PreparedCall(getattr(load(), name), args, (q, k_codes, k_centroids, seq_lens, weights, workspace, f, pages), name)
+
+
+def cq_chunk_weights(q, k_codes, k_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int, weights, decay: float = 1.0,
+                     seq_lens=None, workspace=None, stream=None) -> None:
+    """weights fp32 [B, n_kv_heads, tokens] = decay weights + the causal attention weights of the last m tokens of each sequence,
+    summed over them and over the query heads of each KV head; q fp16 [B, m, Hq, head_dim]."""
+    prepare_chunk_weights(q, k_codes, k_centroids, scale, fmt, t, t_cap, weights, decay, None, seq_lens, workspace)(stream)
+
+
+def cq_chunk_weights_paged(q, k_pool, k_centroids, scale: float, fmt: CQFormat, t: int, pages: PageTable, weights, decay: float = 1.0,
+                           seq_lens=None, workspace=None, stream=None) -> None:
+    """cq_chunk_weights over a paged key pool."""
+    prepare_chunk_weights(q, k_pool, k_centroids, scale, fmt, t, 0, weights, decay, pages, seq_lens, workspace)(stream)
 
 
 def prepare_select_tokens(weights, t: int, keep: int, n_sink: int = 0, n_recent: int = 0, seq_lens=None, kept=None, kept_lens=None):

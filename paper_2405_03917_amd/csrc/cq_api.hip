@@ -1082,6 +1082,85 @@ cq_status cq_chunk_attention_window_paged(const void* q, const void* k_pool, con
                         seq_lens, tokens_per_split, out, workspace, workspace_bytes, stream, nullptr, 0, &w);
 }
 
+namespace {
+
+size_t chunk_weights_stats(const Derived& f, int32_t batch, int32_t n_q_heads, int32_t m, int32_t t, int* row_splits)
+{
+    const int qper = n_q_heads / f.n_kv_heads;
+    *row_splits = chunk_weights_row_splits((t + kTileTokens - 1) / kTileTokens, batch, m * qper, f.n_kv_heads);
+    return sizeof(float2) * (size_t)batch * m * n_q_heads * *row_splits;
+}
+
+cq_status chunk_weights_common(const void* q, const void* k_codes, const void* k_centroids, float scale, const cq_format* fmt,
+                               int32_t batch, int32_t n_q_heads, int32_t m, int32_t t, int32_t t_cap, const cq_page_table* pages,
+                               const int32_t* seq_lens, float* weights, int64_t weights_stride, float decay,
+                               void* workspace, size_t workspace_bytes, void* stream)
+{
+    Derived f;
+    cq_status st = derive(fmt, &f);
+    if (st != CQ_OK) return st;
+    CacheMap map;
+    if (pages) {
+        if ((st = paged_map(f, pages, batch, &map, &t_cap)) != CQ_OK) return st;
+    } else {
+        if (t_cap <= 0 || t_cap % kTileTokens != 0) return CQ_ERR_INVALID_ARG;
+        map = contiguous_map(f, t_cap);
+    }
+    if (!q || !k_codes || !k_centroids || !workspace) return CQ_ERR_INVALID_ARG;
+    if (batch <= 0 || n_q_heads <= 0 || n_q_heads % f.n_kv_heads != 0) return CQ_ERR_INVALID_ARG;
+    if (m <= 0 || t < m || t > t_cap || !std::isfinite(scale)) return CQ_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k_codes) || !aligned16(k_centroids) || !aligned16(workspace)) return CQ_ERR_INVALID_ARG;
+    if ((int64_t)m * n_q_heads > 0x7fffffffLL || (int64_t)batch * f.n_kv_heads > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
+    if ((st = check_weights(Weights{weights, weights_stride, decay}, t)) != CQ_OK) return st;
+    ChunkWeightsArgs a;
+    if (workspace_bytes < chunk_weights_stats(f, batch, n_q_heads, m, t, &a.row_splits)) return CQ_ERR_WORKSPACE_TOO_SMALL;
+    a.q = static_cast<const uint16_t*>(q);
+    a.k_codes = static_cast<const uint8_t*>(k_codes);
+    a.k_centroids = static_cast<const uint16_t*>(k_centroids);
+    a.scale_log2e = scale * 1.4426950408889634f;
+    a.batch = batch;
+    a.m = m;
+    a.n_q_heads = n_q_heads;
+    a.t = t;
+    a.map = map;
+    a.seq_lens = seq_lens;
+    a.stats = static_cast<float2*>(workspace);
+    a.n_split = a.tiles_per_split = 0;
+    a.weights = weights;
+    a.weights_stride = weights_stride;
+    a.decay = decay;
+    a.f = f;
+    return launch_chunk_weights(a, static_cast<hipStream_t>(stream));
+}
+
+}  // namespace
+
+size_t cq_chunk_weights_workspace_bytes(const cq_format* fmt, int32_t batch, int32_t n_q_heads, int32_t m, int32_t t)
+{
+    Derived f;
+    int row_splits;
+    if (derive(fmt, &f) != CQ_OK || batch <= 0 || n_q_heads <= 0 || n_q_heads % f.n_kv_heads != 0 || m <= 0 || t < m) return 0;
+    if ((int64_t)m * n_q_heads > 0x7fffffffLL) return 0;
+    return chunk_weights_stats(f, batch, n_q_heads, m, t, &row_splits);
+}
+
+cq_status cq_chunk_weights(const void* q, const void* k_codes, const void* k_centroids, float scale, const cq_format* fmt,
+                           int32_t batch, int32_t n_q_heads, int32_t m, int32_t t, int32_t t_cap, const int32_t* seq_lens,
+                           float* weights, int64_t weights_stride, float decay, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return chunk_weights_common(q, k_codes, k_centroids, scale, fmt, batch, n_q_heads, m, t, t_cap, nullptr, seq_lens, weights,
+                                weights_stride, decay, workspace, workspace_bytes, stream);
+}
+
+cq_status cq_chunk_weights_paged(const void* q, const void* k_pool, const void* k_centroids, float scale, const cq_format* fmt,
+                                 int32_t batch, int32_t n_q_heads, int32_t m, int32_t t, const cq_page_table* pages, const int32_t* seq_lens,
+                                 float* weights, int64_t weights_stride, float decay, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!pages) return CQ_ERR_INVALID_ARG;
+    return chunk_weights_common(q, k_pool, k_centroids, scale, fmt, batch, n_q_heads, m, t, 0, pages, seq_lens, weights, weights_stride,
+                                decay, workspace, workspace_bytes, stream);
+}
+
 cq_status cq_select_tokens(const float* weights, int64_t weights_stride, int32_t batch, int32_t n_kv_heads, int32_t t,
                            const int32_t* seq_lens, int32_t keep, int32_t n_sink, int32_t n_recent,
                            int32_t* kept, int32_t* kept_lens, void* stream)

@@ -204,6 +204,28 @@ struct DequantArgs {
 };
 cq_status launch_dequantize(const DequantArgs& a, hipStream_t stream);
 
+// Accumulated attention weights of a chunk (cq_chunk_weights.hip).
+struct ChunkWeightsArgs {
+    const uint16_t* q;        // fp16 [batch][m][n_q_heads][head_dim]
+    const uint8_t* k_codes;
+    const uint16_t* k_centroids;
+    float scale_log2e;
+    int batch, m, n_q_heads, t;
+    CacheMap map;
+    const int32_t* seq_lens;
+    int row_splits;           // pieces of the context in the pass over rows, and
+    float2* stats;            // [sequence][KV head][row][row_splits]: (maximum, sum of 2^(score - maximum)) of each
+    int n_split, tiles_per_split;   // pieces of a pass (set by the launcher)
+    float* weights;
+    int64_t weights_stride;
+    float decay;
+    Derived f;
+};
+int chunk_weights_resident(int n_kv_heads);
+int chunk_weights_pieces(int n_tiles, int64_t base, int resident);
+int chunk_weights_row_splits(int n_tiles, int batch, int rows, int n_kv_heads);
+cq_status launch_chunk_weights(const ChunkWeightsArgs& a, hipStream_t stream);
+
 // Eviction (cq_evict.hip): the tokens that stay, per (sequence, KV head) stream, and their move.
 struct SelectArgs {
     const float* weights;     // [stream][weights_stride]
