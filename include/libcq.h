@@ -639,7 +639,8 @@ CQ_API cq_status cq_chunk_weights_paged(const void *q, const void *k_pool, const
  *   kept              out, device int32 [batch][n_kv_heads][keep]: positions in ascending order, -1 behind the last
  *   kept_lens         out, device int32 [batch]: min(t_n, keep), the sequence's length from then on (all its KV heads
  *                     keep as many tokens, each its own)
- * One kernel; the result is a function of the weights alone.
+ *   workspace         device, cq_select_workspace_bytes(...) bytes; may be NULL for t <= 16384
+ * The result is a function of the weights alone.
  *
  * cq_compact_cache   position r of stream (n, h) receives the codes (and, unless both are NULL, the accumulator) of
  * position kept[n][h][r], for r < kept_lens[n].  Accumulators of positions kept_lens[n] .. min(t, t_cap_out) - 1 become
@@ -647,19 +648,21 @@ CQ_API cq_status cq_chunk_weights_paged(const void *q, const void *k_pool, const
  *   k_out, v_out, weights_out   the inputs themselves (in place; t_cap_out = t_cap, weights_out_stride = weights_stride), or
  *                     buffers apart from all others; their old contents behind what is written stay.  keep <= t_cap_out;
  *                     weights_out_stride >= keep and >= min(t, t_cap_out)
- *   kept, kept_lens   device, as written by cq_select_tokens; values outside [0, t) and [0, keep] are clamped
+ *   kept, kept_lens   device, as written by cq_select_tokens; values outside [0, t) and [0, keep] are clamped.  In place, kept[n][h]
+ *                     has to ascend (kept[r] >= r follows); into other buffers it may name any positions in any order
  *   workspace         device, cq_compact_workspace_bytes(...) bytes; may be NULL where no output is an input
  *   Any format, sub-byte ones included.  Keys stay as they are stored: those rotated to their positions keep them, those
  *   cached before the rotary embedding take the positions they move to.
  * cq_compact_cache_paged   the same from the pages of one block table to those of another (the same, or another one over
- * the same pools, or over other pools).  Where pools are the same, everything is read before anything is written.  Two
- * sequences must not share pages that are written.
+ * the same pools, or over other pools).  Where pools are the same and the tables are not, everything is read before anything is
+ * written.  Two sequences must not share pages that are written, nor a sequence name one twice.
  * Errors: CQ_ERR_INVALID_ARG (null, misaligned or overlapping pointers, sizes out of range, more than 65535 streams),
  * CQ_ERR_UNSUPPORTED (format), CQ_ERR_WORKSPACE_TOO_SMALL, CQ_ERR_HIP.
  */
+CQ_API size_t cq_select_workspace_bytes(int32_t batch, int32_t n_kv_heads, int32_t t);
 CQ_API cq_status cq_select_tokens(const float *weights, int64_t weights_stride, int32_t batch, int32_t n_kv_heads, int32_t t,
                            const int32_t *seq_lens, int32_t keep, int32_t n_sink, int32_t n_recent,
-                           int32_t *kept, int32_t *kept_lens, void *stream);
+                           int32_t *kept, int32_t *kept_lens, void *workspace, size_t workspace_bytes, void *stream);
 CQ_API size_t cq_compact_workspace_bytes(const cq_format *fmt, int32_t batch, int32_t keep);
 CQ_API cq_status cq_compact_cache(const void *k_codes, const void *v_codes, const float *weights, int64_t weights_stride, const cq_format *fmt,
                            int32_t batch, int32_t t, int32_t t_cap, const int32_t *kept, const int32_t *kept_lens, int32_t keep,

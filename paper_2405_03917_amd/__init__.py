@@ -39,7 +39,7 @@ EXPORTS = (
     "cq_chunk_window_workspace_bytes", "cq_chunk_attention_window", "cq_chunk_attention_window_paged",
     "cq_decode_weights_workspace_bytes", "cq_decode_attention_weights", "cq_decode_attention_weights_paged",
     "cq_chunk_weights_workspace_bytes", "cq_chunk_weights", "cq_chunk_weights_paged",
-    "cq_select_tokens", "cq_compact_workspace_bytes", "cq_compact_cache", "cq_compact_cache_paged",
+    "cq_select_workspace_bytes", "cq_select_tokens", "cq_compact_workspace_bytes", "cq_compact_cache", "cq_compact_cache_paged",
     "cq_probe_stream_read", "cq_probe_copy", "cq_probe_mfma", "cq_probe_decode_plan",
 )
 
@@ -222,7 +222,9 @@ def load() -> ctypes.CDLL:
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = [vp, vp, vp, f32, fp, i32, i32, i32, i32, at, vp, vp, i64, f32, vp, size, vp]
     lib.cq_select_tokens.restype = ctypes.c_int
-    lib.cq_select_tokens.argtypes = [vp, i64, i32, i32, i32, vp, i32, i32, i32, vp, vp, vp]
+    lib.cq_select_tokens.argtypes = [vp, i64, i32, i32, i32, vp, i32, i32, i32, vp, vp, vp, size, vp]
+    lib.cq_select_workspace_bytes.restype = size
+    lib.cq_select_workspace_bytes.argtypes = [i32, i32, i32]
     lib.cq_compact_workspace_bytes.restype = size
     lib.cq_compact_workspace_bytes.argtypes = [fp, i32, i32]
     for at, name in ((i32, "cq_compact_cache"), (pp, "cq_compact_cache_paged")):
@@ -1383,7 +1385,12 @@ def cq_chunk_weights_paged(q, k_pool, k_centroids, scale: float, fmt: CQFormat, 
     prepare_chunk_weights(q, k_pool, k_centroids, scale, fmt, t, 0, weights, decay, pages, seq_lens, workspace)(stream)
 
 
-def prepare_select_tokens(weights, t: int, keep: int, n_sink: int = 0, n_recent: int = 0, seq_lens=None, kept=None, kept_lens=None):
+def cq_select_workspace_bytes(batch: int, n_kv_heads: int, t: int) -> int:
+    return int(load().cq_select_workspace_bytes(batch, n_kv_heads, t))
+
+
+def prepare_select_tokens(weights, t: int, keep: int, n_sink: int = 0, n_recent: int = 0, seq_lens=None, kept=None, kept_lens=None,
+                          workspace=None):
     """Check and marshal the arguments of cq_select_tokens once.  Returns (call, kept, kept_lens)."""
     import torch
     _dev(weights, torch.float32, "weights")
@@ -1401,16 +1408,19 @@ def prepare_select_tokens(weights, t: int, keep: int, n_sink: int = 0, n_recent:
         _dev(x, torch.int32, what)
         if tuple(x.shape) != shape or not x.is_contiguous():
             raise ValueError(f"{what} must be contiguous int32 {list(shape)}")
-    _same_device(weights, seq_lens, kept, kept_lens)
-    args = (weights.data_ptr(), stride, batch, hkv, t, sl, keep, n_sink, n_recent, kept.data_ptr(), kept_lens.data_ptr())
-    return PreparedCall(load().cq_select_tokens, args, (weights, seq_lens, kept, kept_lens), "cq_select_tokens"), kept, kept_lens
+    workspace = _workspace(workspace, cq_select_workspace_bytes(batch, hkv, t), weights.device, "cq_select_workspace_bytes")
+    _same_device(weights, seq_lens, kept, kept_lens, workspace)
+    args = (weights.data_ptr(), stride, batch, hkv, t, sl, keep, n_sink, n_recent, kept.data_ptr(), kept_lens.data_ptr(),
+            workspace.data_ptr(), workspace.numel())
+    return PreparedCall(load().cq_select_tokens, args, (weights, seq_lens, kept, kept_lens, workspace), "cq_select_tokens"), kept, kept_lens
 
 
-def cq_select_tokens(weights, t: int, keep: int, n_sink: int = 0, n_recent: int = 0, seq_lens=None, kept=None, kept_lens=None, stream=None):
+def cq_select_tokens(weights, t: int, keep: int, n_sink: int = 0, n_recent: int = 0, seq_lens=None, kept=None, kept_lens=None,
+                     workspace=None, stream=None):
     """The `keep` tokens that stay of every sequence and KV head: its first n_sink, its last n_recent, and the heaviest by
     `weights` fp32 [B, n_kv_heads, tokens].  Returns (kept int32 [B, n_kv_heads, keep], ascending, -1 behind the last; kept_lens
     int32 [B], the sequences' new lengths)."""
-    call, kept, kept_lens = prepare_select_tokens(weights, t, keep, n_sink, n_recent, seq_lens, kept, kept_lens)
+    call, kept, kept_lens = prepare_select_tokens(weights, t, keep, n_sink, n_recent, seq_lens, kept, kept_lens, workspace)
     call(stream)
     return kept, kept_lens
 

@@ -1161,15 +1161,32 @@ cq_status cq_chunk_weights_paged(const void* q, const void* k_pool, const void* 
                                 decay, workspace, workspace_bytes, stream);
 }
 
+size_t cq_select_workspace_bytes(int32_t batch, int32_t n_kv_heads, int32_t t)
+{
+    if (batch <= 0 || n_kv_heads <= 0 || t <= 0) return 0;
+    const size_t runs = (size_t)batch * n_kv_heads * (((size_t)t + kSelectRun - 1) / kSelectRun);
+    if (t <= kSelectRun) return 16;
+    return runs * (sizeof(unsigned) * (kSelectCounts + kSelectRun) + sizeof(uint4));
+}
+
 cq_status cq_select_tokens(const float* weights, int64_t weights_stride, int32_t batch, int32_t n_kv_heads, int32_t t,
                            const int32_t* seq_lens, int32_t keep, int32_t n_sink, int32_t n_recent,
-                           int32_t* kept, int32_t* kept_lens, void* stream)
+                           int32_t* kept, int32_t* kept_lens, void* workspace, size_t workspace_bytes, void* stream)
 {
     if (!weights || !kept || !kept_lens || !aligned16(weights) || !aligned16(kept) || !aligned16(kept_lens)) return CQ_ERR_INVALID_ARG;
     if (batch <= 0 || n_kv_heads <= 0 || t <= 0 || weights_stride < t || keep <= 0) return CQ_ERR_INVALID_ARG;
     if (n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > keep) return CQ_ERR_INVALID_ARG;
-    if ((int64_t)batch * n_kv_heads > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
-    const SelectArgs a{weights, weights_stride, seq_lens, batch, n_kv_heads, t, keep, n_sink, n_recent, kept, kept_lens};
+    const int parts = (t - 1) / kSelectRun + 1;
+    const int64_t runs = (int64_t)batch * n_kv_heads * parts;
+    if (runs > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
+    if (parts > 1) {
+        if (!workspace || !aligned16(workspace)) return CQ_ERR_INVALID_ARG;
+        if (workspace_bytes < cq_select_workspace_bytes(batch, n_kv_heads, t)) return CQ_ERR_WORKSPACE_TOO_SMALL;
+    }
+    unsigned* const counts = static_cast<unsigned*>(workspace);
+    unsigned* const lists = parts > 1 ? counts + (size_t)runs * kSelectCounts : nullptr;
+    const SelectArgs a{weights, weights_stride, seq_lens, batch, n_kv_heads, t, keep, n_sink, n_recent, kept, kept_lens,
+                       parts, counts, lists, parts > 1 ? reinterpret_cast<uint4*>(lists + (size_t)runs * kSelectRun) : nullptr};
     return launch_select_tokens(a, static_cast<hipStream_t>(stream));
 }
 
@@ -1226,14 +1243,19 @@ cq_status compact_common(const void* k_codes, const void* v_codes, const float* 
     if (!pages && (same_k || same_v) && t_cap_out != t_cap) return CQ_ERR_INVALID_ARG;
     if (weights && (same_w ? weights_out_stride != weights_stride : overlap(weights_out, wo_bytes, weights, w_bytes))) return CQ_ERR_INVALID_ARG;
     const bool in_place = same_k || same_v || same_w;
+    // Streams that fill the CUs move their tokens forward themselves, in one launch; fewer go through the workspace, where
+    // all CUs take part.
+    const bool same_places = !pages || (pages->block_table == pages_out->block_table && pages->row_stride == pages_out->row_stride &&
+                                        pages->n_pages == pages_out->n_pages);
+    a.slide = same_k && same_v && (!weights || same_w) && same_places && 2 * streams >= 256;
     const size_t codes = round256(compact_codes_bytes(f, batch, keep));
     a.work = nullptr;
     a.work_weights = nullptr;
-    if (in_place) {
+    if (in_place) {                     // (asked for in either case: what a call needs does not follow a choice of kernels)
         if (!workspace) return CQ_ERR_INVALID_ARG;
         if (workspace_bytes < codes + sizeof(float) * streams * keep) return CQ_ERR_WORKSPACE_TOO_SMALL;
-        a.work = static_cast<uint8_t*>(workspace);
-        a.work_weights = reinterpret_cast<float*>(a.work + codes);
+        a.work = a.slide ? nullptr : static_cast<uint8_t*>(workspace);
+        a.work_weights = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + codes);
     }
     a.in[0] = static_cast<const uint8_t*>(k_codes);
     a.in[1] = static_cast<const uint8_t*>(v_codes);
@@ -1249,7 +1271,7 @@ cq_status compact_common(const void* k_codes, const void* v_codes, const float* 
     a.n_kv_heads = f.n_kv_heads;
     a.t = t;
     a.keep = keep;
-    a.t_cap_out = t_cap_out;
+    a.clear_end = weights ? end : 0;
     return launch_compact(a, f, static_cast<hipStream_t>(stream));
 }
 

@@ -20,6 +20,9 @@ constexpr int kSelectThreads = 1024;
 constexpr int kSelectWaves = kSelectThreads / 64;
 constexpr int kDigitBits = 11;                          // three digits: 11, 11, 10 bits
 constexpr int kBins = 1 << kDigitBits;
+constexpr int kPerThread = 16;                          // tokens of a run per thread, in registers
+constexpr int kPart = kSelectThreads * kPerThread;
+static_assert(kPart == kSelectRun, "as the workspace is sized");
 
 // order-preserving: larger weights have larger keys, both zeros the same; what is no number ranks below every number
 __device__ __forceinline__ unsigned weight_key(float w)
@@ -53,68 +56,280 @@ __device__ __forceinline__ unsigned block_prefix(unsigned v, unsigned* sums, int
     return before + x - v;
 }
 
-__global__ __launch_bounds__(kSelectThreads) void select_tokens_kernel(SelectArgs a)
+// The middle of a stream: what is left to choose from once its first and last tokens are kept.
+struct Middle {
+    int t_n, len;                       // tokens of the sequence, between the kept ends (0: nothing to choose)
+    unsigned need;                      // of them, to be chosen
+    const float* w;
+    int32_t* kept;
+};
+__device__ __forceinline__ Middle middle_of(const SelectArgs& a, int stream)
+{
+    const int n = stream / a.n_kv_heads;
+    Middle m;
+    m.t_n = a.t;
+    if (a.seq_lens) m.t_n = min(max(a.seq_lens[n], 0), a.t);
+    m.kept = a.kept + (size_t)stream * a.keep;
+    m.w = a.weights + (size_t)stream * a.weights_stride + a.n_sink;
+    m.need = (unsigned)(a.keep - a.n_sink - a.n_recent);
+    m.len = m.t_n > a.keep && m.need > 0 ? m.t_n - a.n_sink - a.n_recent : 0;
+    return m;
+}
+// What needs no choice: the new length, the ends, short sequences.  (Workgroup `part` of `parts`.)
+__device__ __forceinline__ void keep_ends(const SelectArgs& a, const Middle& m, int stream, int part, int parts, int tid)
+{
+    const int first = part * kSelectThreads + tid, step = parts * kSelectThreads;
+    if (stream % a.n_kv_heads == 0 && first == 0) a.kept_lens[stream / a.n_kv_heads] = min(m.t_n, a.keep);
+    if (m.t_n <= a.keep) {
+        for (int r = first; r < a.keep; r += step) m.kept[r] = r < m.t_n ? r : -1;
+        return;
+    }
+    for (int r = first; r < a.n_sink; r += step) m.kept[r] = r;
+    for (int r = first; r < a.n_recent; r += step) m.kept[a.keep - a.n_recent + r] = m.t_n - a.n_recent + r;
+}
+
+// Keys k of tokens first + 1024 k + thread, of a run of up to kPart tokens, in registers.
+struct Keys {
+    unsigned key[kPerThread];
+    int first, count;                   // tokens of the run
+    __device__ __forceinline__ void load(const Middle& m, int part, int tid)
+    {
+        first = part * kPart;
+        count = min(kPart, m.len - first);
+        float w[kPerThread];
+#pragma unroll
+        for (int k = 0; k < kPerThread; ++k) w[k] = has(k, tid) ? m.w[first + k * kSelectThreads + tid] : 0.f;
+#pragma unroll
+        for (int k = 0; k < kPerThread; ++k) key[k] = weight_key(w[k]);
+    }
+    __device__ __forceinline__ bool has(int k, int tid) const { return k * kSelectThreads + tid < count; }
+    __device__ __forceinline__ bool any(int k) const { return k * kSelectThreads < count; }      // (uniform)
+};
+
+// The bin, from the top, in which `need` is reached, and what is still needed of it: thread i holds bins `hi`, `hi` - 1 =
+// bins - 1 - 2 i and the one below.
+__device__ __forceinline__ void find_bin(unsigned c0, unsigned c1, int hi, unsigned& need, unsigned& bin, unsigned* sums, unsigned* found, int tid)
+{
+    unsigned total;
+    const unsigned above = block_prefix(c0 + c1, sums, tid, &total);
+    if (above < need && above + c0 + c1 >= need) {
+        const bool second = above + c0 < need;
+        found[0] = (unsigned)(second ? hi - 1 : hi);
+        found[1] = need - above - (second ? c0 : 0u);
+    }
+    __syncthreads();
+    bin = found[0];
+    need = found[1];
+    __syncthreads();
+}
+__device__ __forceinline__ void find_bin(const unsigned* hist, int bins, unsigned& need, unsigned& bin, unsigned* sums, unsigned* found, int tid)
+{
+    const int hi = bins - 1 - 2 * tid;
+    find_bin(hi >= 0 ? hist[hi] : 0u, hi >= 1 ? hist[hi - 1] : 0u, hi, need, bin, sums, found, tid);
+}
+__device__ __forceinline__ void clear(unsigned* hist, int tid)
+{
+    for (int i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
+    __syncthreads();
+}
+// The first digits of a run counted in LDS.  Zeros, of which there may be many (tokens that never drew weight), are counted
+// a wavefront at a time: as additions to one word they would wait for each other.
+__device__ __forceinline__ void count_first_digits(const Keys& keys, unsigned* hist, int tid)
+{
+    constexpr unsigned kZero = 0x80000000u;
+    unsigned zeros = 0;
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) {
+        if (!keys.any(k)) break;
+        const bool in = keys.has(k, tid), zero = in && keys.key[k] == kZero;
+        zeros += (unsigned)__builtin_popcountll(__builtin_amdgcn_ballot_w64(zero));
+        if (in && !zero) atomicAdd(&hist[keys.key[k] >> 21], 1u);
+    }
+    if ((tid & 63) == 0 && zeros) atomicAdd(&hist[kZero >> 21], zeros);
+    __syncthreads();
+}
+
+// Positions of the run's tokens whose key is above `key`, or equals it where fewer than `need` equals lie in front, behind
+// gt_base, eq_base such tokens of earlier runs.
+__device__ __forceinline__ void write_kept(const SelectArgs& a, const Middle& m, const Keys& keys, unsigned key, unsigned need, unsigned gt_base,
+                                           unsigned eq_base, unsigned* counts, int tid)
+{
+    static_assert(kPerThread * kSelectWaves == 256, "four counts per lane of a wavefront");
+    const int lane = tid & 63, wave = tid >> 6;
+    const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) {
+        const bool in = keys.has(k, tid);
+        const unsigned gt = (unsigned)__builtin_popcountll(__builtin_amdgcn_ballot_w64(in && keys.key[k] > key));
+        const unsigned eq = (unsigned)__builtin_popcountll(__builtin_amdgcn_ballot_w64(in && keys.key[k] == key));
+        if (lane == 0) counts[k * kSelectWaves + wave] = gt | eq << 16;
+    }
+    __syncthreads();
+    if (wave == 0) {                    // exclusive prefix sums; (equals of a run reach 2^14, so 16 bits hold both)
+        unsigned c[4], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            c[i] = sum;
+            sum += counts[4 * lane + i];
+        }
+        unsigned x = sum;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const unsigned y = __shfl_up(x, d);
+            x += lane >= d ? y : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) counts[4 * lane + i] = c[i] + x - sum;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) {
+        if (!keys.any(k)) break;
+        const bool in = keys.has(k, tid), gt = in && keys.key[k] > key, eq = in && keys.key[k] == key;
+        const unsigned long long gts = __builtin_amdgcn_ballot_w64(gt), eqs = __builtin_amdgcn_ballot_w64(eq);
+        const unsigned at = counts[k * kSelectWaves + wave];
+        const unsigned g = gt_base + (at & 0xffffu) + (unsigned)__builtin_popcountll(gts & below);
+        const unsigned e = eq_base + (at >> 16) + (unsigned)__builtin_popcountll(eqs & below);
+        if (gt || (eq && e < need)) m.kept[a.n_sink + g + min(e, need)] = a.n_sink + keys.first + k * kSelectThreads + tid;
+    }
+}
+
+// Streams of one run: a workgroup each, the keys read once.
+__global__ __launch_bounds__(kSelectThreads) void select_short_kernel(SelectArgs a)
 {
     __shared__ unsigned hist[kBins];
     __shared__ unsigned sums[kSelectWaves];
     __shared__ unsigned found[2];
-    const int tid = threadIdx.x;
-    const int stream = blockIdx.x, n = stream / a.n_kv_heads;
-    int t_n = a.t;
-    if (a.seq_lens) t_n = min(max(a.seq_lens[n], 0), a.t);
-    int32_t* kept = a.kept + (size_t)stream * a.keep;
-    if (stream % a.n_kv_heads == 0 && tid == 0) a.kept_lens[n] = min(t_n, a.keep);
-    if (t_n <= a.keep) {
-        for (int r = tid; r < a.keep; r += kSelectThreads) kept[r] = r < t_n ? r : -1;
-        return;
-    }
-    for (int r = tid; r < a.n_sink; r += kSelectThreads) kept[r] = r;
-    for (int r = tid; r < a.n_recent; r += kSelectThreads) kept[a.keep - a.n_recent + r] = t_n - a.n_recent + r;
-    const float* w = a.weights + (size_t)stream * a.weights_stride + a.n_sink;
-    const int len = t_n - a.n_sink - a.n_recent;            // the tokens between
-    unsigned need = (unsigned)(a.keep - a.n_sink - a.n_recent);
-    if (need == 0) return;
-    // the key of the need-th largest, digit by digit
-    unsigned prefix = 0, mask = 0;
+    const int tid = threadIdx.x, stream = blockIdx.x;
+    const Middle m = middle_of(a, stream);
+    Keys keys;
+    keys.load(m, 0, tid);
+    keep_ends(a, m, stream, 0, 1, tid);
+    if (m.len == 0) return;
+    unsigned need = m.need, bin;
+    clear(hist, tid);
+    count_first_digits(keys, hist, tid);
+    find_bin(hist, kBins, need, bin, sums, found, tid);
+    unsigned prefix = bin << 21, mask = (kBins - 1u) << 21;
 #pragma unroll 1
-    for (int shift = 21; shift >= 0; shift -= shift == 10 ? 10 : 11) {
+    for (int shift = 10; shift >= 0; shift -= 10) {
         const int bins = shift == 0 ? kBins / 2 : kBins;
-        for (int i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < len; i += kSelectThreads) {
-            const unsigned k = weight_key(w[i]);
-            if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
+        clear(hist, tid);
+#pragma unroll
+        for (int k = 0; k < kPerThread; ++k) {
+            if (!keys.any(k)) break;
+            if (keys.has(k, tid) && (keys.key[k] & mask) == prefix) atomicAdd(&hist[(keys.key[k] >> shift) & (bins - 1)], 1u);
         }
         __syncthreads();
-        // thread i holds the bins 2 i, 2 i + 1 from the top; the bin in which `need` is reached
-        const int hi = bins - 1 - 2 * tid;
-        const unsigned c0 = hi >= 0 ? hist[hi] : 0u, c1 = hi >= 1 ? hist[hi - 1] : 0u;
-        unsigned total;
-        const unsigned above = block_prefix(c0 + c1, sums, tid, &total);
-        if (above < need && above + c0 + c1 >= need) {
-            const bool second = above + c0 < need;
-            found[0] = (unsigned)(second ? hi - 1 : hi);
-            found[1] = need - above - (second ? c0 : 0u);
-        }
-        __syncthreads();
-        prefix |= found[0] << shift;
+        find_bin(hist, bins, need, bin, sums, found, tid);
+        prefix |= bin << shift;
         mask |= (unsigned)(bins - 1) << shift;
-        need = found[1];
+    }
+    write_kept(a, m, keys, prefix, need, 0, 0, hist, tid);
+}
+
+// Longer streams: a workgroup per run, three launches.  Each run's first digits are counted; every run then adds up the
+// stream's counts, finds the digit, and lists its keys that have it (in any order: what follows is a function of the set);
+// every run then finds the key among the stream's listed ones, and writes its own tokens.
+// (The listed keys are those of one of 2048 digits: usually some per cent of the stream.  With all weights equal they are the
+// whole stream, read by each of its workgroups.)
+__global__ __launch_bounds__(kSelectThreads) void select_count_kernel(SelectArgs a)
+{
+    __shared__ unsigned hist[kBins];
+    const int tid = threadIdx.x, part = blockIdx.x % a.parts, stream = blockIdx.x / a.parts;
+    const Middle m = middle_of(a, stream);
+    Keys keys;
+    keys.load(m, part, tid);
+    keep_ends(a, m, stream, part, a.parts, tid);
+    if (m.len == 0) return;
+    clear(hist, tid);
+    count_first_digits(keys, hist, tid);
+    unsigned* out = a.counts + (size_t)blockIdx.x * kBins;
+    for (int i = tid; i < kBins; i += kSelectThreads) out[i] = hist[i];
+}
+
+__global__ __launch_bounds__(kSelectThreads) void select_list_kernel(SelectArgs a)
+{
+    __shared__ unsigned sums[kSelectWaves];
+    __shared__ unsigned found[2];
+    __shared__ unsigned listed;
+    const int tid = threadIdx.x, part = blockIdx.x % a.parts, stream = blockIdx.x / a.parts;
+    const Middle m = middle_of(a, stream);
+    if (m.len == 0) return;
+    Keys keys;
+    keys.load(m, part, tid);
+    if (tid == 0) listed = 0;
+    const int hi = kBins - 1 - 2 * tid;
+    const unsigned* all = a.counts + (size_t)stream * a.parts * kBins;
+    unsigned c0 = 0, c1 = 0, mine0 = 0, mine1 = 0;
+    for (int p = 0; p < a.parts; ++p) {
+        const uint2 x = *reinterpret_cast<const uint2*>(all + (size_t)p * kBins + hi - 1);
+        c0 += x.y;
+        c1 += x.x;
+        mine0 = p == part ? x.y : mine0;
+        mine1 = p == part ? x.x : mine1;
+    }
+    unsigned need = m.need, bin;
+    find_bin(c0, c1, hi, need, bin, sums, found, tid);
+    unsigned above;                                         // of this run, with a larger digit
+    block_prefix(((unsigned)hi > bin ? mine0 : 0u) + ((unsigned)(hi - 1) > bin ? mine1 : 0u), sums, tid, &above);
+    unsigned* list = a.lists + (size_t)blockIdx.x * kPart;
+    const int lane = tid & 63;
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) {
+        if (!keys.any(k)) break;
+        const bool mine = keys.has(k, tid) && keys.key[k] >> 21 == bin;
+        const unsigned long long b = __builtin_amdgcn_ballot_w64(mine);
+        unsigned base = 0;
+        if (lane == 0 && b) base = atomicAdd(&listed, (unsigned)__builtin_popcountll(b));
+        base = (unsigned)__builtin_amdgcn_readfirstlane((int)base);
+        if (mine) list[base + (unsigned)__builtin_popcountll(b & ((1ull << lane) - 1))] = keys.key[k];
+    }
+    __syncthreads();
+    if (tid == 0) a.runs[blockIdx.x] = make_uint4(listed, above, bin, need);
+}
+
+__global__ __launch_bounds__(kSelectThreads) void select_write_kernel(SelectArgs a)
+{
+    __shared__ unsigned hist[kBins];
+    __shared__ unsigned sums[kSelectWaves];
+    __shared__ unsigned found[2];
+    const int tid = threadIdx.x, part = blockIdx.x % a.parts, stream = blockIdx.x / a.parts;
+    const Middle m = middle_of(a, stream);
+    if (m.len <= part * kPart) return;
+    Keys keys;
+    keys.load(m, part, tid);
+    const uint4* runs = a.runs + (size_t)stream * a.parts;
+    const unsigned* lists = a.lists + (size_t)stream * a.parts * kPart;
+    const int parts = (m.len + kPart - 1) / kPart;
+    unsigned need = runs[part].w, prefix = runs[part].z << 21, mask = (kBins - 1u) << 21, bin;
+#pragma unroll 1
+    for (int shift = 10; shift >= 0; shift -= 10) {
+        const int bins = shift == 0 ? kBins / 2 : kBins;
+        clear(hist, tid);
+        for (int p = 0; p < parts; ++p)
+            for (unsigned i = tid; i < runs[p].x; i += kSelectThreads) {
+                const unsigned key = lists[(size_t)p * kPart + i];
+                if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (bins - 1)], 1u);
+            }
         __syncthreads();
+        find_bin(hist, bins, need, bin, sums, found, tid);
+        prefix |= bin << shift;
+        mask |= (unsigned)(bins - 1) << shift;
     }
-    // ranks: those above the key, and the first `need` that equal it
-    unsigned gt_base = 0, eq_base = 0;
-    for (int i0 = 0; i0 < len; i0 += kSelectThreads) {
-        const int i = i0 + tid;
-        const unsigned k = i < len ? weight_key(w[i]) : 0u;
-        const bool gt = i < len && k > prefix, eq = i < len && k == prefix;
-        unsigned total;
-        const unsigned at = block_prefix((gt ? 1u : 0u) | (eq ? 0x10000u : 0u), sums, tid, &total);
-        const unsigned gts = gt_base + (at & 0xffffu), eqs = eq_base + (at >> 16);
-        if (gt || (eq && eqs < need)) kept[a.n_sink + gts + min(eqs, need)] = a.n_sink + i;
-        gt_base += total & 0xffffu;
-        eq_base += total >> 16;
+    // what the runs in front of this one keep: those above the key, and those that equal it
+    unsigned gt = 0, eq = 0, gt_base, eq_base;
+    for (int p = 0; p < part; ++p) {
+        if (tid == 0) gt += runs[p].y;
+        for (unsigned i = tid; i < runs[p].x; i += kSelectThreads) {
+            const unsigned key = lists[(size_t)p * kPart + i];
+            gt += key > prefix;
+            eq += key == prefix;
+        }
     }
+    block_prefix(gt, sums, tid, &gt_base);
+    block_prefix(eq, sums, tid, &eq_base);
+    write_kept(a, m, keys, prefix, need, gt_base, eq_base, hist, tid);
 }
 
 // ---------------------------------------------------------------------------------- moving
@@ -168,10 +383,11 @@ struct Record {
     }
 };
 
-// A wavefront moves a tile of one stream of one cache.  GATHER: from a token's old position to its new one (in the caches,
-// or in the workspace where the caches' own places are still to be read); else from the workspace to the caches.
+// A wavefront moves a tile of one stream of one cache, or (tiles behind the last that is kept) clears its accumulators.
+// GATHER: from a token's old position to its new one (in the caches, or in the workspace where the caches' own places are
+// still to be read); else from the workspace to the caches.
 template <int GH, int B, bool GATHER>
-__global__ __launch_bounds__(kMoveThreads) void move_tokens_kernel(CompactArgs a, int tiles, int64_t items)
+__global__ __launch_bounds__(kMoveThreads) void move_tokens_kernel(CompactArgs a, int tiles, int work_tiles, int64_t items)
 {
     constexpr int TILE = kTileTokens * GH * B / 8;
     const int lane = threadIdx.x & 63;
@@ -183,62 +399,115 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens_kernel(CompactArgs a
     const int n = stream / a.n_kv_heads, h = stream % a.n_kv_heads;
     const int count = min(max(a.kept_lens[n], 0), a.keep);
     const int r = tile * kTileTokens + lane;
-    uint8_t* const work = a.work ? a.work + ((size_t)item) * TILE : nullptr;
-    float* const work_weights = a.work_weights ? a.work_weights + (size_t)stream * a.keep : nullptr;
+    float* const weights_out = a.weights_out + (size_t)stream * a.weights_out_stride;
     if (r < count) {
+        uint8_t* const work = a.work ? a.work + (((size_t)stream * work_tiles + tile) * 2 + which) * TILE : nullptr;
+        float* const work_weights = a.work_weights + (size_t)stream * a.keep;
         Record<GH, B> rec;
         uint8_t* const out = work && GATHER ? work : a.out[which] + a.map_out.tile_index(n, h, tile) * TILE;
         if constexpr (GATHER) {
             const int from = min(max(a.kept[(size_t)stream * a.keep + r], 0), a.t - 1);
             rec.load(a.in[which] + a.map_in.tile_index(n, h, from / kTileTokens) * TILE, from % kTileTokens);
-            rec.move(from % kTileTokens, lane);
             if (which == 0 && a.weights) {
                 const float x = a.weights[(size_t)stream * a.weights_stride + from];
                 if (work) work_weights[r] = x;
-                else a.weights_out[(size_t)stream * a.weights_out_stride + r] = x;
+                else weights_out[r] = x;
             }
+            rec.move(from % kTileTokens, lane);
         } else {
             rec.load(work, lane);
-            if (which == 0 && a.weights) a.weights_out[(size_t)stream * a.weights_out_stride + r] = work_weights[r];
+            if (which == 0 && a.weights) weights_out[r] = work_weights[r];
         }
         rec.store(out, lane);
+    } else if (which == 0 && a.weights && r < a.clear_end && (!a.work || !GATHER)) {
+        weights_out[r] = 0.f;
     }
 }
 
-// accumulators behind the tokens that stay: zero, up to `end`
-__global__ __launch_bounds__(kMoveThreads) void clear_weights_kernel(CompactArgs a, int end)
+// In place, a workgroup per stream of one cache: a token moves towards the front and the list ascends, so a block of tokens
+// that is read before it is written overwrites nothing that a later one reads.  The next block is on its way meanwhile.
+constexpr int kSlideThreads = 512;
+template <int GH, int B>
+__global__ __launch_bounds__(kSlideThreads) void slide_tokens_kernel(CompactArgs a)
 {
-    const int stream = blockIdx.y, n = stream / a.n_kv_heads;
+    constexpr int TILE = kTileTokens * GH * B / 8;
+    const int tid = threadIdx.x, which = blockIdx.x & 1, stream = blockIdx.x >> 1;
+    const int n = stream / a.n_kv_heads, h = stream % a.n_kv_heads;
     const int count = min(max(a.kept_lens[n], 0), a.keep);
-    const int i = blockIdx.x * kMoveThreads + threadIdx.x;
-    if (i >= count && i < end) a.weights_out[(size_t)stream * a.weights_out_stride + i] = 0.f;
+    const int32_t* kept = a.kept + (size_t)stream * a.keep;
+    const bool weigh = which == 0 && a.weights;
+    uint8_t* const codes = a.out[which];
+    float* const weights = a.weights_out + (size_t)stream * a.weights_out_stride;
+    auto source = [&](int r) { return r < count ? min(max(kept[r], 0), a.t - 1) : r; };
+    struct Token {
+        Record<GH, B> rec;
+        float w;
+        int from;
+    };
+    auto load = [&](Token& x, int r, int from) {
+        x.from = from;
+        if (from != r) {                                    // (tokens in front of the first that goes stay where they are)
+            x.rec.load(codes + a.map_out.tile_index(n, h, from / kTileTokens) * TILE, from % kTileTokens);
+            if (weigh) x.w = weights[from];
+        }
+    };
+    Token now, next;
+    load(now, tid, source(tid));
+    int from_next = source(kSlideThreads + tid);
+#pragma unroll 1
+    for (int base = 0; base < count; base += kSlideThreads) {
+        const int r = base + tid;
+        load(next, r + kSlideThreads, from_next);
+        from_next = source(r + 2 * kSlideThreads);
+        const bool moves = now.from != r;
+        if (moves) {
+            now.rec.move(now.from % kTileTokens, r % kTileTokens);
+            asm volatile("" :: "v"(now.rec.w[0]), "v"(now.rec.w[GH / 4 - 1]), "v"(now.rec.hi), "v"(now.w) : "memory");   // (all of it is here)
+        }
+        lds_barrier();                                      // the block is read
+        if (moves) {
+            now.rec.store(codes + a.map_out.tile_index(n, h, r / kTileTokens) * TILE, r % kTileTokens);
+            if (weigh) weights[r] = now.w;
+        }
+        now = next;
+    }
+    if (weigh)
+        for (int r = count + tid; r < a.clear_end; r += kSlideThreads) weights[r] = 0.f;
 }
 
 template <int GH, int B>
 cq_status launch_move(const CompactArgs& a, hipStream_t stream)
 {
-    const int tiles = (a.keep + kTileTokens - 1) / kTileTokens;
-    const int64_t items = (int64_t)2 * a.batch * a.n_kv_heads * tiles, wgs = (items + kMoveThreads / 64 - 1) / (kMoveThreads / 64);
-    if (wgs > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
-    hipLaunchKernelGGL((move_tokens_kernel<GH, B, true>), dim3((unsigned)wgs), dim3(kMoveThreads), 0, stream, a, tiles, items);
-    if (hipGetLastError() != hipSuccess) return CQ_ERR_HIP;
-    if (a.work) {
-        hipLaunchKernelGGL((move_tokens_kernel<GH, B, false>), dim3((unsigned)wgs), dim3(kMoveThreads), 0, stream, a, tiles, items);
+    const int streams = a.batch * a.n_kv_heads;
+    if (a.slide) {
+        hipLaunchKernelGGL((slide_tokens_kernel<GH, B>), dim3(2u * (unsigned)streams), dim3(kSlideThreads), 0, stream, a);
+        return hipGetLastError() == hipSuccess ? CQ_OK : CQ_ERR_HIP;
+    }
+    const int work_tiles = (a.keep + kTileTokens - 1) / kTileTokens, end_tiles = (a.clear_end + kTileTokens - 1) / kTileTokens;
+    for (int pass = 0; pass < (a.work ? 2 : 1); ++pass) {
+        const bool last = !a.work || pass == 1;
+        const int tiles = last && a.weights && end_tiles > work_tiles ? end_tiles : work_tiles;
+        const int64_t items = (int64_t)2 * streams * tiles, wgs = (items + kMoveThreads / 64 - 1) / (kMoveThreads / 64);
+        if (wgs > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
+        if (pass == 0) hipLaunchKernelGGL((move_tokens_kernel<GH, B, true>), dim3((unsigned)wgs), dim3(kMoveThreads), 0, stream, a, tiles, work_tiles, items);
+        else hipLaunchKernelGGL((move_tokens_kernel<GH, B, false>), dim3((unsigned)wgs), dim3(kMoveThreads), 0, stream, a, tiles, work_tiles, items);
         if (hipGetLastError() != hipSuccess) return CQ_ERR_HIP;
     }
-    if (!a.weights) return CQ_OK;
-    const int end = a.t < a.t_cap_out ? a.t : a.t_cap_out;
-    const int streams = a.batch * a.n_kv_heads;
-    if (streams > 65535) return CQ_ERR_INVALID_ARG;
-    hipLaunchKernelGGL(clear_weights_kernel, dim3((unsigned)((end + kMoveThreads - 1) / kMoveThreads), (unsigned)streams), dim3(kMoveThreads), 0, stream, a, end);
-    return hipGetLastError() == hipSuccess ? CQ_OK : CQ_ERR_HIP;
+    return CQ_OK;
 }
 
 }  // namespace
 
 cq_status launch_select_tokens(const SelectArgs& a, hipStream_t stream)
 {
-    hipLaunchKernelGGL(select_tokens_kernel, dim3((unsigned)(a.batch * a.n_kv_heads)), dim3(kSelectThreads), 0, stream, a);
+    const unsigned grid = (unsigned)(a.batch * a.n_kv_heads) * (unsigned)a.parts;
+    if (a.parts == 1) {
+        hipLaunchKernelGGL(select_short_kernel, dim3(grid), dim3(kSelectThreads), 0, stream, a);
+    } else {
+        hipLaunchKernelGGL(select_count_kernel, dim3(grid), dim3(kSelectThreads), 0, stream, a);
+        hipLaunchKernelGGL(select_list_kernel, dim3(grid), dim3(kSelectThreads), 0, stream, a);
+        hipLaunchKernelGGL(select_write_kernel, dim3(grid), dim3(kSelectThreads), 0, stream, a);
+    }
     return hipGetLastError() == hipSuccess ? CQ_OK : CQ_ERR_HIP;
 }
 

@@ -234,7 +234,15 @@ struct SelectArgs {
     int batch, n_kv_heads, t, keep, n_sink, n_recent;
     int32_t* kept;            // [stream][keep]: ascending positions, -1 behind the last
     int32_t* kept_lens;       // [sequence]
+    // streams of more than kSelectRun tokens: a workgroup per run of that many (`parts` of them), and in the workspace
+    // each run's counts of first digits, its listed keys, and (listed, above, digit, needed)
+    int parts;
+    unsigned* counts;
+    unsigned* lists;
+    uint4* runs;
 };
+constexpr int kSelectRun = 16384;
+constexpr int kSelectCounts = 2048;
 cq_status launch_select_tokens(const SelectArgs& a, hipStream_t stream);
 
 struct CompactArgs {
@@ -247,7 +255,9 @@ struct CompactArgs {
     int64_t weights_out_stride;
     const int32_t* kept;
     const int32_t* kept_lens;
-    int batch, n_kv_heads, t, keep, t_cap_out;
+    int batch, n_kv_heads, t, keep;
+    int clear_end;            // accumulators behind the tokens that stay become zero up to here
+    bool slide;               // every output is its input, place by place: a workgroup per stream moves its tokens forward
     // what is read may be written (null: it is not): the tokens go here first, tile by tile as the caches hold them
     uint8_t* work;
     float* work_weights;
