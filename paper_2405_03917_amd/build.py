@@ -21,8 +21,9 @@ FLAGS = [
 ]
 
 
-# per-file additions: the MFMA filter's running maxima must not be canonicalised (its header says why)
-FILE_FLAGS = {"cq_encode_mfma.hip": ["-fno-honor-nans"], "cq_kmeans_mfma.hip": ["-fno-honor-nans"]}
+# per-file additions: running maxima over products of the matrix cores must not be canonicalised (an instruction each; the
+# MFMA filter's header says more)
+FILE_FLAGS = {"cq_encode_mfma.hip": ["-fno-honor-nans"], "cq_kmeans_mfma.hip": ["-fno-honor-nans"], "cq_chunk_weights.hip": ["-fno-honor-nans"]}
 
 
 def build(verbose: bool = True) -> str:

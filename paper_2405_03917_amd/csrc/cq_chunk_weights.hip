@@ -11,6 +11,8 @@
 // 256 query rows in LDS; a wavefront takes 64-token tiles by itself, gathers their keys from the codebook straight into the
 // operand of S^T = K Q^T (v_mfma_f32_32x32x16_f16: a lane's 8 channels are the centroids of its token's codes) and keeps
 // them for all row blocks.  Every sum has a fixed order: equal calls give equal bits.
+#include <type_traits>
+
 #include "cq_key_gather.hpp"
 #include "cq_lds_gather.hpp"
 
@@ -26,10 +28,11 @@ constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBlockRows = 32;
 constexpr int kGroupRows = 256;                         // query rows in LDS at a time
-// LDS: key codebook, query rows of 256 bytes (their 16-byte pieces exchanged by the row's low bits), per row (M, 1 / L) and
+// LDS: key codebook, query rows, per row (M, 1 / L) and
 // its position, the wavefronts' (maximum, sum) pairs, a word of each wavefront
 constexpr unsigned kQueries = kBookBytes;
-constexpr unsigned kRowStats = kQueries + kGroupRows * 256;
+constexpr unsigned kQueryStride = 272;                  // (256 + 16: eight rows' pieces lie in different banks)
+constexpr unsigned kRowStats = kQueries + kGroupRows * kQueryStride;
 constexpr unsigned kRowPos = kRowStats + kGroupRows * 8;
 constexpr unsigned kWavePairs = kRowPos + kGroupRows * 4;
 constexpr unsigned kFlags = kWavePairs + kWaves * kGroupRows * 8;
@@ -102,22 +105,21 @@ struct TileKeys {
     }
 };
 
-// What a wavefront does with a block of 32 rows: scores of the tile's 64 tokens, lane (rc, kh) row rc,
-// acc[tb][i] token 32 tb + 8 (i / 4) + 4 kh + i % 4.
-template <int GH, int C, int B>
-__device__ __forceinline__ void block_scores(const TileKeys<GH, C, B>& keys, int rb, int rc, int kh, float16_t (&acc)[2])
+// A block of 32 query rows as B operands: lane (rc, kh) holds channels 16 s + 8 kh .. + 7 of row rc in q[s].
+__device__ __forceinline__ half8_t read_query(int rb, int s, int rc, int kh)
 {
-#pragma unroll
-    for (int tb = 0; tb < 2; ++tb)
+    return lds_half8((unsigned)rc * kQueryStride + (unsigned)kh * 16 + (unsigned)rb * (kBlockRows * kQueryStride) + kQueries + (unsigned)s * 32);
+}
+// One of 16 products of a block's scores of the tile's 64 tokens: acc[tb][i] is token 32 tb + 8 (i / 4) + 4 kh + i % 4, query rc.
+template <int GH, int C, int B>
+__device__ __forceinline__ void product(const TileKeys<GH, C, B>& keys, const half8_t (&q)[8], float16_t (&acc)[2], int k)
+{
+    const int s = k >> 1, tb = k & 1;
+    if (s == 0) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[tb][i] = 0.f;
-    const unsigned row = kQueries + (unsigned)(rb * kBlockRows + rc) * 256;
-#pragma unroll
-    for (int s = 0; s < 8; ++s) {
-        const half8_t q = lds_half8(row + (unsigned)((2 * s + kh) ^ (rc & 15)) * 16);
-        acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(keys.kv[0][s], q, acc[0], 0, 0, 0);
-        acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(keys.kv[1][s], q, acc[1], 0, 0, 0);
     }
+    acc[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(keys.kv[tb][s], q[s], acc[tb], 0, 0, 0);
 }
 
 // Sum over the 32 lanes of a half-wavefront of 32 values each: lane rc receives the sum of value rc.
@@ -200,7 +202,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
                 const int row = min(row0 + r, rows - 1), j = row / qper;
                 u32x4 w = *reinterpret_cast<const u32x4*>(a.q + (((size_t)n * a.m + j) * a.n_q_heads + hkv * qper + (row - j * qper)) * D + piece * 8);
                 w ^= flip;
-                *(lds_q*)(kQueries + (unsigned)r * 256 + (unsigned)(piece ^ (r & 15)) * 16) = w;
+                *(lds_q*)(kQueries + (unsigned)r * kQueryStride + (unsigned)piece * 16) = w;
                 float mine = 0.f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -235,65 +237,114 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
             const bool large = __builtin_amdgcn_ballot_w64(lane < kWaves && *(lds_i*)(kFlags + (unsigned)(lane & (kWaves - 1)) * 4) != 0) != 0;
             const float mult = large ? 1.f : scale, early = large ? scale : 1.f;
 
-            float ref[NB], l[NB];
-#pragma unroll
-            for (int rb = 0; rb < NB; ++rb) {
-                ref[rb] = kNoScore;
-                l[rb] = 0.f;
+            if constexpr (!COLUMNS) {
+                for (int r = lane; r < kRows; r += 64) *(lds_f2*)(kWavePairs + (unsigned)(wave * kGroupRows + r) * 8) = float2_t{kNoScore, 0.f};
+                asm volatile("" ::: "memory");              // (a wavefront's LDS operations keep their order)
             }
 #pragma unroll 1
             for (; tile < tile1; tile += kWaves) {
+                half8_t q[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) q[k] = read_query(0, k, rc, kh);
                 keys.gather(ck_head, rc, kh);
                 keys.request(tile_at(tile + kWaves), rc);
                 const bool hides = large || tile * kTileTokens + kTileTokens - 1 > pos0;
                 auto mask = [&](int rb, float16_t (&acc)[2]) {
                     if (!hides) return;
-                    const int pos = *(lds_i*)(kRowPos + (unsigned)(rb * kBlockRows + rc) * 4);
+                    const int rel = *(lds_i*)(kRowPos + (unsigned)(rb * kBlockRows + rc) * 4) - tile * kTileTokens - 4 * kh;
 #pragma unroll
-                    for (int tb = 0; tb < 2; ++tb) {
-                        const int tok0 = tile * kTileTokens + tb * 32 + 4 * kh;
+                    for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[tb][i] = tok0 + 8 * (i >> 2) + (i & 3) <= pos ? acc[tb][i] * early : -INFINITY;
+                        for (int i = 0; i < 16; ++i) acc[tb][i] = rel >= 32 * tb + 8 * (i >> 2) + (i & 3) ? acc[tb][i] * early : -INFINITY;
+                };
+                // The vector work on a block's scores goes slice by slice between the products of the next block, and behind each
+                // product's operand the same one of the block after it is requested.
+                auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+                auto between = [&](int rb, float16_t (&next)[2], auto last, auto&& slice) {
+                    const int after = min(rb + 2, blocks - 1);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        if constexpr (!decltype(last)::value) {
+                            product(keys, q, next, k);
+                            if (k & 1) q[k >> 1] = read_query(after, k >> 1, rc, kh);
+                        }
+                        slice(k);
+                        fence();
                     }
                 };
-                if constexpr (!COLUMNS) {
+                float16_t acc[2][2];
+                fence();
 #pragma unroll
-                    for (int rb = 0; rb < NB; ++rb) {
-                        if (rb < blocks) {
-                            float16_t acc[2];
-                            block_scores(keys, rb, rc, kh, acc);
-                            mask(rb, acc);
-                            float top = -INFINITY;
+                for (int k = 0; k < 16; ++k) product(keys, q, acc[0], k);
+                fence();
+                if constexpr (NB > 1) {
 #pragma unroll
-                            for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) top = fmaxf(top, acc[tb][i]);
-                            const float next = fmaxf(ref[rb], top * mult);
-                            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                            for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) sum[i & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[tb][i], mult, -next));
-                            l[rb] = __builtin_fmaf(l[rb], __builtin_amdgcn_exp2f(ref[rb] - next), (sum[0] + sum[1]) + (sum[2] + sum[3]));
-                            ref[rb] = next;
-                        }
-                    }
-                } else {
-                    float col[32];
+                    for (int k = 0; k < 8; ++k) q[k] = read_query(min(1, blocks - 1), k, rc, kh);
+                }
+                fence();
+                float col[32];
+                if constexpr (COLUMNS) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) col[i] = 0.f;
-#pragma unroll 1
-                    for (int rb = 0; rb < blocks; ++rb) {
-                        float16_t acc[2];
-                        block_scores(keys, rb, rc, kh, acc);
-                        mask(rb, acc);
+                }
+                auto here = [](float& v) { asm volatile("" : "+v"(v)); };   // (formed here, not where it is next used)
+                auto value = [&](float16_t (&x)[2], int i) { return x[i >> 4][i & 15]; };
+                auto block = [&](int rb, float16_t (&x)[2], float16_t (&next)[2], auto last) {
+                    mask(rb, x);
+                    if constexpr (!COLUMNS) {
+                        // (a row's two half-wavefronts share reference and sum)
+                        const unsigned at = kWavePairs + (unsigned)(wave * kGroupRows + rb * kBlockRows + rc) * 8;
+                        const float2_t old = *(lds_f2*)at;
+                        float top = -INFINITY, ref = 0.f, alpha = 0.f, sum[2] = {0.f, 0.f};
+                        between(rb, next, last, [&](int k) {
+                            if (k < 4) {
+#pragma unroll
+                                for (int i = 8 * k; i < 8 * k + 8; i += 2) top = fmaxf(top, fmaxf(value(x, i), value(x, i + 1)));
+                                here(top);
+                            } else if (k == 4) {
+                                const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+                                ref = fmaxf(old[0], fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * mult);
+                                alpha = __builtin_amdgcn_exp2f(old[0] - ref);
+                                here(alpha);
+                            } else {
+#pragma unroll
+                                for (int i = 3 * (k - 5); i < 3 * (k - 5) + 3 && i < 32; ++i)
+                                    sum[i & 1] += __builtin_amdgcn_exp2f(__builtin_fmaf(value(x, i), mult, -ref));
+                                here(sum[0]);
+                                here(sum[1]);
+                            }
+                        });
+                        const float mine = sum[0] + sum[1];
+                        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mine), __float_as_uint(mine), false, false);
+                        if (kh == 0) *(lds_f2*)at = float2_t{ref, __builtin_fmaf(old[1], alpha, __uint_as_float(r[0]) + __uint_as_float(r[1]))};
+                    } else {
                         const float2_t st = *(lds_f2*)(kRowStats + (unsigned)(rb * kBlockRows + rc) * 8);
+                        between(rb, next, last, [&](int k) {
 #pragma unroll
-                        for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i)
-                                col[16 * tb + i] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(acc[tb][i], mult, -st[0])), st[1], col[16 * tb + i]);
+                            for (int i = 2 * k; i < 2 * k + 2; ++i)
+                                col[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(value(x, i), mult, -st[0])), st[1], col[i]);
+                            here(col[2 * k]);
+                            here(col[2 * k + 1]);
+                        });
                     }
+                };
+                if constexpr (NB == 1) {
+                    block(0, acc[0], acc[1], std::true_type{});
+                } else {
+                    int rb = 0;
+#pragma unroll 1
+                    for (; rb + 2 < blocks; rb += 2) {
+                        block(rb, acc[0], acc[1], std::false_type{});
+                        block(rb + 1, acc[1], acc[0], std::false_type{});
+                    }
+                    if (rb + 1 < blocks) {
+                        block(rb, acc[0], acc[1], std::false_type{});
+                        block(rb + 1, acc[1], acc[0], std::true_type{});
+                    } else {
+                        block(rb, acc[0], acc[1], std::true_type{});
+                    }
+                }
+                if constexpr (COLUMNS) {
                     const float sum = sum_over_rows(col, rc);
                     const int tok = tile * kTileTokens + (rc >> 4) * 32 + 8 * (rc >> 2 & 3) + 4 * kh + (rc & 3);
                     if (tok < t_n) {
@@ -303,18 +354,11 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
                 }
             }
             if constexpr (!COLUMNS) {
-                // ---- the half-wavefronts' and the wavefronts' pairs of every row
+                // ---- the wavefronts' pairs of every row
                 auto merged = [](float m0, float l0, float m1, float l1) {
                     const float m = fmaxf(m0, m1);
                     return float2_t{m, __builtin_fmaf(l0, __builtin_amdgcn_exp2f(m0 - m), l1 * __builtin_amdgcn_exp2f(m1 - m))};
                 };
-#pragma unroll
-                for (int rb = 0; rb < NB; ++rb) {
-                    const auto mr = __builtin_amdgcn_permlane32_swap(__float_as_uint(ref[rb]), __float_as_uint(ref[rb]), false, false);
-                    const auto lr = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[rb]), __float_as_uint(l[rb]), false, false);
-                    const float2_t x = merged(__uint_as_float(mr[0]), __uint_as_float(lr[0]), __uint_as_float(mr[1]), __uint_as_float(lr[1]));
-                    if (kh == 0) *(lds_f2*)(kWavePairs + (unsigned)(wave * kGroupRows + rb * kBlockRows + rc) * 8) = x;
-                }
                 lds_barrier();
                 for (int r = tid; r < kRows && row0 + r < rows; r += kThreads) {
                     float2_t x = *(lds_f2*)(kWavePairs + (unsigned)r * 8);
@@ -358,7 +402,6 @@ cq_status launch_rows(const ChunkWeightsArgs& a, hipStream_t stream)
 {
     const int blocks = (a.m * (a.n_q_heads / a.f.n_kv_heads) + kBlockRows - 1) / kBlockRows;
     if (blocks <= 1) return launch_passes<GH, C, B, 1>(a, stream);
-    if (blocks <= 4) return launch_passes<GH, C, B, 4>(a, stream);
     return launch_passes<GH, C, B, 8>(a, stream);
 }
 
