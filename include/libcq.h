@@ -639,7 +639,7 @@ CQ_API cq_status cq_chunk_weights_paged(const void *q, const void *k_pool, const
  *   kept              out, device int32 [batch][n_kv_heads][keep]: positions in ascending order, -1 behind the last
  *   kept_lens         out, device int32 [batch]: min(t_n, keep), the sequence's length from then on (all its KV heads
  *                     keep as many tokens, each its own)
- *   workspace         device, cq_select_workspace_bytes(...) bytes; may be NULL for t <= 16384
+ *   workspace         device, cq_select_workspace_bytes(...) bytes; may be NULL for t <= 8192
  * The result is a function of the weights alone.
  *
  * cq_compact_cache   position r of stream (n, h) receives the codes (and, unless both are NULL, the accumulator) of

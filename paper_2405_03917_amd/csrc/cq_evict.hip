@@ -16,12 +16,12 @@ namespace cq {
 namespace {
 
 // ---------------------------------------------------------------------------------- selection
-constexpr int kSelectThreads = 1024;
-constexpr int kSelectWaves = kSelectThreads / 64;
+constexpr int kSelectThreads = 512;                     // of a run of a long stream
 constexpr int kDigitBits = 11;                          // three digits: 11, 11, 10 bits
 constexpr int kBins = 1 << kDigitBits;
 constexpr int kPerThread = 16;                          // tokens of a run per thread, in registers
 constexpr int kPart = kSelectThreads * kPerThread;
+constexpr int kListRoom = 8192;                         // listed keys of a stream that fit in LDS (32 KB)
 static_assert(kPart == kSelectRun, "as the workspace is sized");
 
 // order-preserving: larger weights have larger keys, both zeros the same; what is no number ranks below every number
@@ -32,9 +32,11 @@ __device__ __forceinline__ unsigned weight_key(float w)
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// exclusive prefix sum over the workgroup's threads; *total: the sum
+// exclusive prefix sum over the workgroup's NT threads; *total: the sum
+template <int NT>
 __device__ __forceinline__ unsigned block_prefix(unsigned v, unsigned* sums, int tid, unsigned* total)
 {
+    constexpr int kSelectWaves = NT / 64;
     const int lane = tid & 63, wave = tid >> 6;
     unsigned x = v;
 #pragma unroll
@@ -76,9 +78,10 @@ __device__ __forceinline__ Middle middle_of(const SelectArgs& a, int stream)
     return m;
 }
 // What needs no choice: the new length, the ends, short sequences.  (Workgroup `part` of `parts`.)
+template <int NT>
 __device__ __forceinline__ void keep_ends(const SelectArgs& a, const Middle& m, int stream, int part, int parts, int tid)
 {
-    const int first = part * kSelectThreads + tid, step = parts * kSelectThreads;
+    const int first = part * NT + tid, step = parts * NT;
     if (stream % a.n_kv_heads == 0 && first == 0) a.kept_lens[stream / a.n_kv_heads] = min(m.t_n, a.keep);
     if (m.t_n <= a.keep) {
         for (int r = first; r < a.keep; r += step) m.kept[r] = r < m.t_n ? r : -1;
@@ -88,53 +91,68 @@ __device__ __forceinline__ void keep_ends(const SelectArgs& a, const Middle& m, 
     for (int r = first; r < a.n_recent; r += step) m.kept[a.keep - a.n_recent + r] = m.t_n - a.n_recent + r;
 }
 
-// Keys k of tokens first + 1024 k + thread, of a run of up to kPart tokens, in registers.
+// Keys k of tokens first + NT k + thread, of a run of up to 16 NT tokens, in registers.
+template <int NT>
 struct Keys {
     unsigned key[kPerThread];
     int first, count;                   // tokens of the run
     __device__ __forceinline__ void load(const Middle& m, int part, int tid)
     {
-        first = part * kPart;
-        count = min(kPart, m.len - first);
+        first = part * (NT * kPerThread);
+        count = min(NT * kPerThread, m.len - first);
         float w[kPerThread];
 #pragma unroll
-        for (int k = 0; k < kPerThread; ++k) w[k] = has(k, tid) ? m.w[first + k * kSelectThreads + tid] : 0.f;
+        for (int k = 0; k < kPerThread; ++k) w[k] = has(k, tid) ? m.w[first + k * NT + tid] : 0.f;
 #pragma unroll
         for (int k = 0; k < kPerThread; ++k) key[k] = weight_key(w[k]);
     }
-    __device__ __forceinline__ bool has(int k, int tid) const { return k * kSelectThreads + tid < count; }
-    __device__ __forceinline__ bool any(int k) const { return k * kSelectThreads < count; }      // (uniform)
+    __device__ __forceinline__ bool has(int k, int tid) const { return k * NT + tid < count; }
+    __device__ __forceinline__ bool any(int k) const { return k * NT < count; }      // (uniform)
 };
 
-// The bin, from the top, in which `need` is reached, and what is still needed of it: thread i holds bins `hi`, `hi` - 1 =
-// bins - 1 - 2 i and the one below.
-__device__ __forceinline__ void find_bin(unsigned c0, unsigned c1, int hi, unsigned& need, unsigned& bin, unsigned* sums, unsigned* found, int tid)
+// The bin, from the top, in which `need` is reached, and what is still needed of it: thread i holds bins hi, hi - 1, ... (N of
+// them), hi = bins - 1 - N i.
+template <int NT, int N>
+__device__ __forceinline__ void find_among(const unsigned (&c)[N], int hi, unsigned& need, unsigned& bin, unsigned* sums, unsigned* found, int tid)
 {
-    unsigned total;
-    const unsigned above = block_prefix(c0 + c1, sums, tid, &total);
-    if (above < need && above + c0 + c1 >= need) {
-        const bool second = above + c0 < need;
-        found[0] = (unsigned)(second ? hi - 1 : hi);
-        found[1] = need - above - (second ? c0 : 0u);
+    unsigned sum = 0, total;
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum += c[i];
+    unsigned above = block_prefix<NT>(sum, sums, tid, &total);
+    if (above < need && above + sum >= need) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (above < need && above + c[i] >= need) {
+                found[0] = (unsigned)(hi - i);
+                found[1] = need - above;
+            }
+            above += c[i];
+        }
     }
     __syncthreads();
     bin = found[0];
     need = found[1];
-    __syncthreads();
 }
+template <int NT>
 __device__ __forceinline__ void find_bin(const unsigned* hist, int bins, unsigned& need, unsigned& bin, unsigned* sums, unsigned* found, int tid)
 {
-    const int hi = bins - 1 - 2 * tid;
-    find_bin(hi >= 0 ? hist[hi] : 0u, hi >= 1 ? hist[hi - 1] : 0u, hi, need, bin, sums, found, tid);
+    constexpr int N = kBins / NT;
+    const int hi = bins - 1 - N * tid;
+    unsigned c[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) c[i] = hi - i >= 0 ? hist[hi - i] : 0u;
+    find_among<NT, N>(c, hi, need, bin, sums, found, tid);
 }
+template <int NT>
 __device__ __forceinline__ void clear(unsigned* hist, int tid)
 {
-    for (int i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
+    for (int i = tid; i < kBins / 4; i += NT) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
 }
 // The first digits of a run counted in LDS.  Zeros, of which there may be many (tokens that never drew weight), are counted
 // a wavefront at a time: as additions to one word they would wait for each other.
-__device__ __forceinline__ void count_first_digits(const Keys& keys, unsigned* hist, int tid)
+template <int NT>
+__device__ __forceinline__ void count_first_digits(const Keys<NT>& keys, unsigned* hist, int tid)
 {
     constexpr unsigned kZero = 0x80000000u;
     unsigned zeros = 0;
@@ -151,10 +169,11 @@ __device__ __forceinline__ void count_first_digits(const Keys& keys, unsigned* h
 
 // Positions of the run's tokens whose key is above `key`, or equals it where fewer than `need` equals lie in front, behind
 // gt_base, eq_base such tokens of earlier runs.
-__device__ __forceinline__ void write_kept(const SelectArgs& a, const Middle& m, const Keys& keys, unsigned key, unsigned need, unsigned gt_base,
+template <int NT>
+__device__ __forceinline__ void write_kept(const SelectArgs& a, const Middle& m, const Keys<NT>& keys, unsigned key, unsigned need, unsigned gt_base,
                                            unsigned eq_base, unsigned* counts, int tid)
 {
-    static_assert(kPerThread * kSelectWaves == 256, "four counts per lane of a wavefront");
+    constexpr int kWaves = NT / 64, N = kPerThread * kWaves / 64;      // counts per lane of a wavefront
     const int lane = tid & 63, wave = tid >> 6;
     const unsigned long long below = (1ull << lane) - 1;
 #pragma unroll
@@ -162,15 +181,15 @@ __device__ __forceinline__ void write_kept(const SelectArgs& a, const Middle& m,
         const bool in = keys.has(k, tid);
         const unsigned gt = (unsigned)__builtin_popcountll(__builtin_amdgcn_ballot_w64(in && keys.key[k] > key));
         const unsigned eq = (unsigned)__builtin_popcountll(__builtin_amdgcn_ballot_w64(in && keys.key[k] == key));
-        if (lane == 0) counts[k * kSelectWaves + wave] = gt | eq << 16;
+        if (lane == 0) counts[k * kWaves + wave] = gt | eq << 16;
     }
     __syncthreads();
-    if (wave == 0) {                    // exclusive prefix sums; (equals of a run reach 2^14, so 16 bits hold both)
-        unsigned c[4], sum = 0;
+    if (wave == 0) {                    // exclusive prefix sums; (equals of a run reach 2^13: 16 bits hold both)
+        unsigned c[N], sum = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < N; ++i) {
             c[i] = sum;
-            sum += counts[4 * lane + i];
+            sum += counts[N * lane + i];
         }
         unsigned x = sum;
 #pragma unroll
@@ -179,7 +198,7 @@ __device__ __forceinline__ void write_kept(const SelectArgs& a, const Middle& m,
             x += lane >= d ? y : 0u;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) counts[4 * lane + i] = c[i] + x - sum;
+        for (int i = 0; i < N; ++i) counts[N * lane + i] = c[i] + x - sum;
     }
     __syncthreads();
 #pragma unroll
@@ -187,62 +206,64 @@ __device__ __forceinline__ void write_kept(const SelectArgs& a, const Middle& m,
         if (!keys.any(k)) break;
         const bool in = keys.has(k, tid), gt = in && keys.key[k] > key, eq = in && keys.key[k] == key;
         const unsigned long long gts = __builtin_amdgcn_ballot_w64(gt), eqs = __builtin_amdgcn_ballot_w64(eq);
-        const unsigned at = counts[k * kSelectWaves + wave];
+        const unsigned at = counts[k * kWaves + wave];
         const unsigned g = gt_base + (at & 0xffffu) + (unsigned)__builtin_popcountll(gts & below);
         const unsigned e = eq_base + (at >> 16) + (unsigned)__builtin_popcountll(eqs & below);
-        if (gt || (eq && e < need)) m.kept[a.n_sink + g + min(e, need)] = a.n_sink + keys.first + k * kSelectThreads + tid;
+        if (gt || (eq && e < need)) m.kept[a.n_sink + g + min(e, need)] = a.n_sink + keys.first + k * NT + tid;
     }
 }
 
 // Streams of one run: a workgroup each, the keys read once.
-__global__ __launch_bounds__(kSelectThreads) void select_short_kernel(SelectArgs a)
+template <int NT>
+__global__ __launch_bounds__(NT) void select_short_kernel(SelectArgs a)
 {
-    __shared__ unsigned hist[kBins];
-    __shared__ unsigned sums[kSelectWaves];
+    __shared__ __align__(16) unsigned hist[kBins];
+    __shared__ unsigned sums[NT / 64];
     __shared__ unsigned found[2];
     const int tid = threadIdx.x, stream = blockIdx.x;
     const Middle m = middle_of(a, stream);
-    Keys keys;
+    Keys<NT> keys;
     keys.load(m, 0, tid);
-    keep_ends(a, m, stream, 0, 1, tid);
+    keep_ends<NT>(a, m, stream, 0, 1, tid);
     if (m.len == 0) return;
     unsigned need = m.need, bin;
-    clear(hist, tid);
+    clear<NT>(hist, tid);
     count_first_digits(keys, hist, tid);
-    find_bin(hist, kBins, need, bin, sums, found, tid);
+    find_bin<NT>(hist, kBins, need, bin, sums, found, tid);
     unsigned prefix = bin << 21, mask = (kBins - 1u) << 21;
 #pragma unroll 1
     for (int shift = 10; shift >= 0; shift -= 10) {
         const int bins = shift == 0 ? kBins / 2 : kBins;
-        clear(hist, tid);
+        clear<NT>(hist, tid);
 #pragma unroll
         for (int k = 0; k < kPerThread; ++k) {
             if (!keys.any(k)) break;
             if (keys.has(k, tid) && (keys.key[k] & mask) == prefix) atomicAdd(&hist[(keys.key[k] >> shift) & (bins - 1)], 1u);
         }
         __syncthreads();
-        find_bin(hist, bins, need, bin, sums, found, tid);
+        find_bin<NT>(hist, bins, need, bin, sums, found, tid);
         prefix |= bin << shift;
         mask |= (unsigned)(bins - 1) << shift;
     }
-    write_kept(a, m, keys, prefix, need, 0, 0, hist, tid);
+    __syncthreads();
+    write_kept<NT>(a, m, keys, prefix, need, 0, 0, hist, tid);
 }
 
 // Longer streams: a workgroup per run, three launches.  Each run's first digits are counted; every run then adds up the
 // stream's counts, finds the digit, and lists its keys that have it (in any order: what follows is a function of the set);
 // every run then finds the key among the stream's listed ones, and writes its own tokens.
-// (The listed keys are those of one of 2048 digits: usually some per cent of the stream.  With all weights equal they are the
-// whole stream, read by each of its workgroups.)
+// (The listed keys are those of one of 2048 digits, usually less than a hundredth of the stream, and are taken to LDS.  With all
+// weights equal they are the whole stream, read from memory by each of its workgroups.)
 __global__ __launch_bounds__(kSelectThreads) void select_count_kernel(SelectArgs a)
 {
-    __shared__ unsigned hist[kBins];
+    __shared__ __align__(16) unsigned hist[kBins];
     const int tid = threadIdx.x, part = blockIdx.x % a.parts, stream = blockIdx.x / a.parts;
     const Middle m = middle_of(a, stream);
-    Keys keys;
+    Keys<kSelectThreads> keys;
     keys.load(m, part, tid);
-    keep_ends(a, m, stream, part, a.parts, tid);
+    keep_ends<kSelectThreads>(a, m, stream, part, a.parts, tid);
     if (m.len == 0) return;
-    clear(hist, tid);
+    clear<kSelectThreads>(hist, tid);
     count_first_digits(keys, hist, tid);
     unsigned* out = a.counts + (size_t)blockIdx.x * kBins;
     for (int i = tid; i < kBins; i += kSelectThreads) out[i] = hist[i];
@@ -250,40 +271,48 @@ __global__ __launch_bounds__(kSelectThreads) void select_count_kernel(SelectArgs
 
 __global__ __launch_bounds__(kSelectThreads) void select_list_kernel(SelectArgs a)
 {
-    __shared__ unsigned sums[kSelectWaves];
+    __shared__ unsigned sums[kSelectThreads / 64];
     __shared__ unsigned found[2];
     __shared__ unsigned listed;
     const int tid = threadIdx.x, part = blockIdx.x % a.parts, stream = blockIdx.x / a.parts;
     const Middle m = middle_of(a, stream);
     if (m.len == 0) return;
-    Keys keys;
+    Keys<kSelectThreads> keys;
     keys.load(m, part, tid);
     if (tid == 0) listed = 0;
-    const int hi = kBins - 1 - 2 * tid;
+    static_assert(kBins == 4 * kSelectThreads, "four bins a thread");
+    const int hi = kBins - 1 - 4 * tid;
     const unsigned* all = a.counts + (size_t)stream * a.parts * kBins;
-    unsigned c0 = 0, c1 = 0, mine0 = 0, mine1 = 0;
+    unsigned c[4] = {0, 0, 0, 0}, mine[4] = {0, 0, 0, 0};
+#pragma unroll 4
     for (int p = 0; p < a.parts; ++p) {
-        const uint2 x = *reinterpret_cast<const uint2*>(all + (size_t)p * kBins + hi - 1);
-        c0 += x.y;
-        c1 += x.x;
-        mine0 = p == part ? x.y : mine0;
-        mine1 = p == part ? x.x : mine1;
+        const uint4 x = *reinterpret_cast<const uint4*>(all + (size_t)p * kBins + hi - 3);
+        const unsigned down[4] = {x.w, x.z, x.y, x.x};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            c[i] += down[i];
+            mine[i] = p == part ? down[i] : mine[i];
+        }
     }
     unsigned need = m.need, bin;
-    find_bin(c0, c1, hi, need, bin, sums, found, tid);
+    find_among<kSelectThreads, 4>(c, hi, need, bin, sums, found, tid);
     unsigned above;                                         // of this run, with a larger digit
-    block_prefix(((unsigned)hi > bin ? mine0 : 0u) + ((unsigned)(hi - 1) > bin ? mine1 : 0u), sums, tid, &above);
+    unsigned larger = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) larger += (unsigned)(hi - i) > bin ? mine[i] : 0u;
+    block_prefix<kSelectThreads>(larger, sums, tid, &above);
     unsigned* list = a.lists + (size_t)blockIdx.x * kPart;
     const int lane = tid & 63;
 #pragma unroll
     for (int k = 0; k < kPerThread; ++k) {
         if (!keys.any(k)) break;
-        const bool mine = keys.has(k, tid) && keys.key[k] >> 21 == bin;
-        const unsigned long long b = __builtin_amdgcn_ballot_w64(mine);
+        const bool in = keys.has(k, tid) && keys.key[k] >> 21 == bin;
+        const unsigned long long b = __builtin_amdgcn_ballot_w64(in);
+        if (b == 0) continue;
         unsigned base = 0;
-        if (lane == 0 && b) base = atomicAdd(&listed, (unsigned)__builtin_popcountll(b));
+        if (lane == 0) base = atomicAdd(&listed, (unsigned)__builtin_popcountll(b));
         base = (unsigned)__builtin_amdgcn_readfirstlane((int)base);
-        if (mine) list[base + (unsigned)__builtin_popcountll(b & ((1ull << lane) - 1))] = keys.key[k];
+        if (in) list[base + (unsigned)__builtin_popcountll(b & ((1ull << lane) - 1))] = keys.key[k];
     }
     __syncthreads();
     if (tid == 0) a.runs[blockIdx.x] = make_uint4(listed, above, bin, need);
@@ -291,45 +320,91 @@ __global__ __launch_bounds__(kSelectThreads) void select_list_kernel(SelectArgs 
 
 __global__ __launch_bounds__(kSelectThreads) void select_write_kernel(SelectArgs a)
 {
-    __shared__ unsigned hist[kBins];
-    __shared__ unsigned sums[kSelectWaves];
+    __shared__ __align__(16) unsigned hist[kBins];
+    __shared__ unsigned sums[kSelectThreads / 64];
     __shared__ unsigned found[2];
+    __shared__ unsigned held[kListRoom];
+    __shared__ unsigned starts[67];                         // of the first 64 runs; of this one; of all; the larger digits in front
     const int tid = threadIdx.x, part = blockIdx.x % a.parts, stream = blockIdx.x / a.parts;
     const Middle m = middle_of(a, stream);
     if (m.len <= part * kPart) return;
-    Keys keys;
+    Keys<kSelectThreads> keys;
     keys.load(m, part, tid);
     const uint4* runs = a.runs + (size_t)stream * a.parts;
     const unsigned* lists = a.lists + (size_t)stream * a.parts * kPart;
     const int parts = (m.len + kPart - 1) / kPart;
     unsigned need = runs[part].w, prefix = runs[part].z << 21, mask = (kBins - 1u) << 21, bin;
+    // where each run's listed keys begin among the stream's; what the runs in front of this one keep with a larger digit
+    if (tid < 64) {
+        unsigned base = 0, gts = 0;
+        for (int p0 = 0; p0 < parts; p0 += 64) {
+            const uint4 r = p0 + tid < parts ? runs[p0 + tid] : make_uint4(0, 0, 0, 0);
+            unsigned x = r.x;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const unsigned y = __shfl_up(x, d);
+                x += tid >= d ? y : 0u;
+            }
+            if (p0 == 0) starts[tid] = base + x - r.x;
+            if (part >= p0 && part < p0 + 64 && tid == part - p0) starts[64] = base + x - r.x;
+            gts += wave_sum_u32(p0 + tid < part ? r.y : 0u);
+            base += (unsigned)__builtin_amdgcn_readlane((int)x, 63);
+        }
+        if (tid == 0) {
+            starts[65] = base;
+            starts[66] = gts;
+        }
+    }
+    __syncthreads();
+    const unsigned before = starts[64], listed = starts[65], gt_runs = starts[66];
+    const bool in_lds = parts <= 64 && listed <= kListRoom;     // (uniform)
+    if (in_lds) {
+        for (unsigned i = tid; i < listed; i += kSelectThreads) {
+            int p = 0;
+            while (p + 1 < parts && starts[p + 1] <= i) ++p;
+            held[i] = lists[(size_t)p * kPart + (i - starts[p])];
+        }
+    }
+    // every listed key with its number in the stream's lists, run by run
+    auto each = [&](auto&& f) {
+        unsigned base = 0;
+        for (int p = 0; p < parts; ++p) {
+            const unsigned n = runs[p].x;
+            for (unsigned i = tid; i < n; i += kSelectThreads) f(base + i, lists[(size_t)p * kPart + i]);
+            base += n;
+        }
+    };
+    auto again = [&](auto&& f) {
+        if (in_lds) {
+            for (unsigned i = tid; i < listed; i += kSelectThreads) f(i, held[i]);
+        } else {
+            each(f);
+        }
+    };
 #pragma unroll 1
     for (int shift = 10; shift >= 0; shift -= 10) {
         const int bins = shift == 0 ? kBins / 2 : kBins;
-        clear(hist, tid);
-        for (int p = 0; p < parts; ++p)
-            for (unsigned i = tid; i < runs[p].x; i += kSelectThreads) {
-                const unsigned key = lists[(size_t)p * kPart + i];
-                if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (bins - 1)], 1u);
-            }
+        clear<kSelectThreads>(hist, tid);
+        again([&](unsigned, unsigned key) {
+            if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (bins - 1)], 1u);
+        });
         __syncthreads();
-        find_bin(hist, bins, need, bin, sums, found, tid);
+        find_bin<kSelectThreads>(hist, bins, need, bin, sums, found, tid);
         prefix |= bin << shift;
         mask |= (unsigned)(bins - 1) << shift;
     }
     // what the runs in front of this one keep: those above the key, and those that equal it
-    unsigned gt = 0, eq = 0, gt_base, eq_base;
-    for (int p = 0; p < part; ++p) {
-        if (tid == 0) gt += runs[p].y;
-        for (unsigned i = tid; i < runs[p].x; i += kSelectThreads) {
-            const unsigned key = lists[(size_t)p * kPart + i];
-            gt += key > prefix;
-            eq += key == prefix;
-        }
+    unsigned gt = 0, eq = 0, gt_base = 0, eq_base = 0;
+    if (part > 0) {                                         // (uniform)
+        again([&](unsigned i, unsigned key) {
+            gt += i < before && key > prefix;
+            eq += i < before && key == prefix;
+        });
+        block_prefix<kSelectThreads>(gt, sums, tid, &gt_base);
+        block_prefix<kSelectThreads>(eq, sums, tid, &eq_base);
     }
-    block_prefix(gt, sums, tid, &gt_base);
-    block_prefix(eq, sums, tid, &eq_base);
-    write_kept(a, m, keys, prefix, need, gt_base, eq_base, hist, tid);
+    __syncthreads();
+    write_kept<kSelectThreads>(a, m, keys, prefix, need, gt_runs + gt_base, eq_base, hist, tid);
 }
 
 // ---------------------------------------------------------------------------------- moving
@@ -387,18 +462,17 @@ struct Record {
 // GATHER: from a token's old position to its new one (in the caches, or in the workspace where the caches' own places are
 // still to be read); else from the workspace to the caches.
 template <int GH, int B, bool GATHER>
-__global__ __launch_bounds__(kMoveThreads) void move_tokens_kernel(CompactArgs a, int tiles, int work_tiles, int64_t items)
+__global__ __launch_bounds__(kMoveThreads) void move_tokens_kernel(CompactArgs a, int tiles, int work_tiles)
 {
     constexpr int TILE = kTileTokens * GH * B / 8;
     const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * (kMoveThreads / 64) + (threadIdx.x >> 6);
-    if (item >= items) return;
-    const int which = (int)(item & 1);
-    const int64_t rest = item >> 1;
-    const int tile = (int)(rest % tiles), stream = (int)(rest / tiles);
+    const int tile = (int)blockIdx.x * (kMoveThreads / 64) + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (tile >= tiles) return;
+    const int stream = blockIdx.y, which = blockIdx.z;
     const int n = stream / a.n_kv_heads, h = stream % a.n_kv_heads;
-    const int count = min(max(a.kept_lens[n], 0), a.keep);
     const int r = tile * kTileTokens + lane;
+    int from = a.kept[(size_t)stream * a.keep + min(r, a.keep - 1)];       // (requested with the length)
+    const int count = min(max(a.kept_lens[n], 0), a.keep);
     float* const weights_out = a.weights_out + (size_t)stream * a.weights_out_stride;
     if (r < count) {
         uint8_t* const work = a.work ? a.work + (((size_t)stream * work_tiles + tile) * 2 + which) * TILE : nullptr;
@@ -406,7 +480,7 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens_kernel(CompactArgs a
         Record<GH, B> rec;
         uint8_t* const out = work && GATHER ? work : a.out[which] + a.map_out.tile_index(n, h, tile) * TILE;
         if constexpr (GATHER) {
-            const int from = min(max(a.kept[(size_t)stream * a.keep + r], 0), a.t - 1);
+            from = min(max(from, 0), a.t - 1);
             rec.load(a.in[which] + a.map_in.tile_index(n, h, from / kTileTokens) * TILE, from % kTileTokens);
             if (which == 0 && a.weights) {
                 const float x = a.weights[(size_t)stream * a.weights_stride + from];
@@ -487,10 +561,9 @@ cq_status launch_move(const CompactArgs& a, hipStream_t stream)
     for (int pass = 0; pass < (a.work ? 2 : 1); ++pass) {
         const bool last = !a.work || pass == 1;
         const int tiles = last && a.weights && end_tiles > work_tiles ? end_tiles : work_tiles;
-        const int64_t items = (int64_t)2 * streams * tiles, wgs = (items + kMoveThreads / 64 - 1) / (kMoveThreads / 64);
-        if (wgs > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
-        if (pass == 0) hipLaunchKernelGGL((move_tokens_kernel<GH, B, true>), dim3((unsigned)wgs), dim3(kMoveThreads), 0, stream, a, tiles, work_tiles, items);
-        else hipLaunchKernelGGL((move_tokens_kernel<GH, B, false>), dim3((unsigned)wgs), dim3(kMoveThreads), 0, stream, a, tiles, work_tiles, items);
+        const dim3 grid((unsigned)((tiles + kMoveThreads / 64 - 1) / (kMoveThreads / 64)), (unsigned)streams, 2);
+        if (pass == 0) hipLaunchKernelGGL((move_tokens_kernel<GH, B, true>), grid, dim3(kMoveThreads), 0, stream, a, tiles, work_tiles);
+        else hipLaunchKernelGGL((move_tokens_kernel<GH, B, false>), grid, dim3(kMoveThreads), 0, stream, a, tiles, work_tiles);
         if (hipGetLastError() != hipSuccess) return CQ_ERR_HIP;
     }
     return CQ_OK;
@@ -502,7 +575,7 @@ cq_status launch_select_tokens(const SelectArgs& a, hipStream_t stream)
 {
     const unsigned grid = (unsigned)(a.batch * a.n_kv_heads) * (unsigned)a.parts;
     if (a.parts == 1) {
-        hipLaunchKernelGGL(select_short_kernel, dim3(grid), dim3(kSelectThreads), 0, stream, a);
+        hipLaunchKernelGGL(select_short_kernel<kSelectThreads>, dim3(grid), dim3(kSelectThreads), 0, stream, a);
     } else {
         hipLaunchKernelGGL(select_count_kernel, dim3(grid), dim3(kSelectThreads), 0, stream, a);
         hipLaunchKernelGGL(select_list_kernel, dim3(grid), dim3(kSelectThreads), 0, stream, a);

@@ -241,7 +241,7 @@ struct SelectArgs {
     unsigned* lists;
     uint4* runs;
 };
-constexpr int kSelectRun = 16384;
+constexpr int kSelectRun = 8192;
 constexpr int kSelectCounts = 2048;
 cq_status launch_select_tokens(const SelectArgs& a, hipStream_t stream);
 
