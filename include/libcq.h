@@ -583,9 +583,9 @@ CQ_API cq_status cq_chunk_attention_window_paged(const void *q, const void *k_po
  *   workspace         device, cq_decode_weights_workspace_bytes(...) bytes (partials, and the scores in fp32)
  *   everything else as in cq_decode_attention, and the output as there.
  * Weights are fp32, from fp32 scores; each accumulator is formed by one thread in a fixed order (no atomics), so equal
- * calls give equal bits.  Two launches.
+ * calls give equal bits.
  * Errors: as cq_decode_attention; CQ_ERR_INVALID_ARG also for weights null or misaligned, weights_stride < t or a decay
- * that is not finite.
+ * that is not finite; CQ_ERR_UNSUPPORTED for more than 4096 query heads to a KV head.
  */
 CQ_API size_t cq_decode_weights_workspace_bytes(const cq_format *fmt, int32_t batch, int32_t n_q_heads, int32_t t, int32_t tokens_per_split);
 CQ_API cq_status cq_decode_attention_weights(const void *q, const void *k_codes, const void *v_codes,

@@ -538,6 +538,7 @@ cq_status decode_common(const void* q, const void* x_k_new, const void* x_v_new,
     Window win = window ? *window : Window{0, 0};
     if (window && (st = check_window(&win, t)) != CQ_OK) return st;
     if (weights && (st = check_weights(*weights, t)) != CQ_OK) return st;
+    if (weights && n_q_heads / f.n_kv_heads > kMaxWeightHeads) return CQ_ERR_UNSUPPORTED;
     const int max_tiles = rope ? decode_rope_max_tiles_per_split() : decode_max_tiles_per_split(f);
     const int n_tiles = view_tiles(t, 1, win.window, win.n_sink);
     const int tiles = tokens_per_split ? tokens_per_split / kTileTokens
@@ -589,6 +590,7 @@ cq_status decode_common(const void* q, const void* x_k_new, const void* x_v_new,
     a.weights = weights ? weights->acc : nullptr;
     a.weights_stride = weights ? weights->stride : 0;
     a.decay = weights ? weights->decay : 0.f;
+    a.finish = false;
     if (rope) return launch_decode_rope(a, static_cast<const float*>(rope_table), rope_positions, static_cast<hipStream_t>(stream));
     if (window || weights) return launch_decode_view(a, static_cast<hipStream_t>(stream));
     return launch_decode(a, static_cast<hipStream_t>(stream));
@@ -984,6 +986,7 @@ cq_status chunk_common(const void* q, const void* k_codes, const void* v_codes,
             a.window = win.window;
             a.n_sink = win.n_sink;
             a.scores = nullptr;
+            a.finish = false;
             st = window ? launch_decode_view(a, static_cast<hipStream_t>(stream)) : launch_decode(a, static_cast<hipStream_t>(stream));
             if (st != CQ_OK) return st;
         }

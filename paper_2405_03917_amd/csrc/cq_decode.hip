@@ -400,14 +400,22 @@ cq_status launch_decode_view(const DecodeViewArgs& a_in, hipStream_t stream)
 {
     DecodeViewArgs a = a_in;
     if (decode_takes_quads(a_in, view_tiles(a_in.t, 1, a_in.window, a_in.n_sink), &a)) return launch_decode_quad_view(a, stream);
-    // (with the scores kept, a kernel of its own reads them when the last split is done, and merges there)
-    a.merge_counters = a.n_split > 1 && !a.scores ? g_merge_counters.for_stream(stream, a.batch * a.n_q_heads) : nullptr;
+    // With the scores kept, the weights need all splits of a row and all query heads of a KV head.  One query head and a short
+    // context, or one of medium length where other rows' workgroups run meanwhile: the row's last workgroup adds them up as it merges
+    // the output.  Otherwise a kernel of its own, which merges too.  32 heads, a kernel of its own -> here, us:
+    // CQ-8c8b 1 x 100 11.5 -> 8.0, 1 x 2000 12.5 -> 10.8, 1 x 4096 12.9 -> 11.5, 1 x 8192 13.5 -> 14.7, 1 x 16384 17.2 -> 23.1, 8 x 2000 15.6 ->
+    // 12.3, 8 x 16384 45.2 -> 40.8, 32 x 4096 46.9 -> 43.2; CQ-4c8b 8 x 4096 23.8 -> 21.7; CQ-2c8b 1 x 1000 16.0 -> 14.0, 8 x 8192 61.5 -> 61.2;
+    // CQ-8c10b 1 x 1000 18.8 -> 15.7, 8 x 8192 41.2 -> 41.4.
+    const int rows = a.batch * a.n_q_heads;
+    const bool short_rows = a.scores && a.n_q_heads == a.f.n_kv_heads && (a.t <= 4096 || (a.t <= 16384 && rows >= 256));
+    a.merge_counters = a.n_split > 1 && (!a.scores || short_rows) ? g_merge_counters.for_stream(stream, a.batch * a.n_q_heads) : nullptr;
+    a.finish = short_rows && (a.n_split == 1 || a.merge_counters);
     const cq_status st = decode_takes_pairs(a) ? launch_decode_pair_view(a, stream)
                          : a.scores        ? launch_format<false, false, kScores>(a, stream)
                          : a.xk_new        ? launch_format<true, false, kWindow>(a, stream)
                                            : launch_format<false, false, kWindow>(a, stream);
-    if (st == CQ_OK && a.scores) return launch_decode_weights(a, stream);
-    if (st != CQ_OK || a.n_split == 1 || a.merge_counters) return st;
+    if (st == CQ_OK && a.scores && !a.finish) return launch_decode_weights(a, stream);
+    if (st != CQ_OK || a.n_split == 1 || a.merge_counters || a.finish) return st;
     return launch_decode_merge(a, stream);
 }
 

@@ -50,21 +50,6 @@ struct Seen<kWindow> {
     __device__ __forceinline__ bool token(int tok, int t_n) const { return tok < t_n && (tok >= first || tok < n_sink); }
 };
 
-// kScores: the score of a row's token to memory.
-template <int VIEW, class Args>
-__device__ __forceinline__ void keep_score(const Args& a, size_t row, int tok, float s)
-{
-    if constexpr (VIEW == kScores) a.scores[row * a.score_stride + tok] = s;
-}
-
-// kScores: a split's reference and sum.  (The sum of the probabilities in fixed point, by which the output is divided, is no
-// substitute: equal probabilities of a long context are all rounded the same way, 1e-4 of their sum at 131072 tokens.)
-template <int VIEW, class Args>
-__device__ __forceinline__ void keep_stats(const Args& a, size_t row, int split, float m, float l)
-{
-    if constexpr (VIEW == kScores) a.stats[row * a.n_split + split] = make_float2(m, l);
-}
-
 // LayerPtrs as the kernel reads it.  A pointer read from memory could point anywhere (LDS,
 // scratch) as far as the compiler knows, and every access through it would be a flat instruction,
 // which waits on the LDS counter and the memory counter at once; the table's pointers are
@@ -120,6 +105,69 @@ __device__ __forceinline__ void partial_store(float* p, float v)
 {
     __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+// kScores: the score of a row's token to memory (where other workgroups of the running kernel read it, device-scope).
+template <int VIEW, class Args>
+__device__ __forceinline__ void keep_score(const Args& a, size_t row, int tok, float s)
+{
+    if constexpr (VIEW == kScores) {
+        float* const at = a.scores + row * a.score_stride + tok;
+        if (a.finish) partial_store(at, s);
+        else *at = s;
+    }
+}
+// kScores: a split's reference and sum.  (The sum of the probabilities in fixed point, by which the output is divided, is no
+// substitute: equal probabilities of a long context are all rounded the same way, 1e-4 of their sum at 131072 tokens.)
+template <int VIEW, class Args>
+__device__ __forceinline__ void keep_stats(const Args& a, size_t row, int split, float m, float l)
+{
+    if constexpr (VIEW == kScores) {
+        float* const at = reinterpret_cast<float*>(a.stats + row * a.n_split + split);
+        partial_store(at, m);
+        partial_store(at + 1, l);
+    }
+}
+// A row's softmax reference and the reciprocal of its sum, from those of its splits (by a wavefront).
+template <bool DEVICE_LOADS>
+__device__ __forceinline__ float2 row_stats(const DecodeViewArgs& a, size_t row, int lane)
+{
+    const float* p = reinterpret_cast<const float*>(a.stats + row * a.n_split);
+    float m = -INFINITY;
+    for (int s = lane; s < a.n_split; s += 64) m = fmaxf(m, partial_load<DEVICE_LOADS>(p + 2 * s));
+    m = wave_max(m);
+    float l = 0.f;
+    for (int s = lane; s < a.n_split; s += 64)
+        l = __builtin_fmaf(partial_load<DEVICE_LOADS>(p + 2 * s + 1), __builtin_amdgcn_exp2f(partial_load<DEVICE_LOADS>(p + 2 * s) - m), l);
+    l = wave_sum(l);
+    return make_float2(m, 1.f / l);
+}
+// The accumulators of a KV head with one query head, by a workgroup, once all of the row's scores and statistics are written.
+template <int VIEW, class Args>
+__device__ __forceinline__ void finish_weights(const Args& a, size_t row, int t_n, int tid, int nt)
+{
+    if constexpr (VIEW == kScores) {
+        constexpr int N = 8;                                // tokens of a thread that are requested together
+        const float* s = a.scores + row * a.score_stride;
+        float* acc = a.weights + row * a.weights_stride;
+        float2 st;
+        for (int base = 0; base < t_n; base += N * nt) {       // (uniform: row_stats exchanges between all lanes)
+            float score[N], old[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const int tok = base + tid + k * nt;
+                score[k] = tok < t_n ? partial_load<true>(s + tok) : 0.f;
+                old[k] = a.decay != 0.f && tok < t_n ? acc[tok] : 0.f;
+            }
+            if (base == 0) st = row_stats<true>(a, row, tid & 63);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const int tok = base + tid + k * nt;
+                const float w = __builtin_fmaf(__builtin_amdgcn_exp2f(score[k] - st.x), st.y, 0.f);
+                if (tok < t_n) acc[tok] = __builtin_fmaf(a.decay, old[k], w);
+            }
+        }
+    }
+}
+
 // The last split of a (sequence, query head) to finish merges them all.  Partials are written with device-scope
 // stores (write-through) and the merging workgroup reads them with device-scope loads, so
 // no cache has to be written back or invalidated as a whole (a device-scope release fence

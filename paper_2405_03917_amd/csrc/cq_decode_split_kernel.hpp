@@ -125,6 +125,9 @@ __global__ __launch_bounds__(kDecodeThreads, 4) void decode_split_kernel(DecodeA
         if (!a.merge_counters || !counted_last<D>(a, part, sums, tid)) return;
         merge_splits<true>(part - (size_t)split * (D + kPartialHeader), a.n_split, D,
                            out_ptr + (size_t)n * out_batch_stride + (size_t)hq * D, tid, NT);
+#if CQ_VIEW_KERNEL
+        if (a.finish) finish_weights<VIEW>(a, (size_t)n * a.n_q_heads + hq, t_n, tid, NT);
+#endif
     };
     if (tile0 >= tile1) {               // this split lies beyond the sequence: neutral partial
 #if CQ_VIEW_KERNEL
@@ -344,9 +347,6 @@ __global__ __launch_bounds__(kDecodeThreads, 4) void decode_split_kernel(DecodeA
         // (the sum is formed here, behind its gathers: left free, the compiler sinks the additions of
         // all tiles of a chunk behind the last tile and runs out of registers for the gathered words)
         asm volatile("" : "+v"(sv));
-#if CQ_VIEW_KERNEL
-        keep_score<VIEW>(a, (size_t)n * a.n_q_heads + hq, tok, sv);
-#endif
         const float m_new = fmaxf(lane_m, sv);
         lane_l = __builtin_fmaf(lane_l, __builtin_amdgcn_exp2f(lane_m - m_new), __builtin_amdgcn_exp2f(sv - m_new));
         lane_m = m_new;
@@ -355,6 +355,10 @@ __global__ __launch_bounds__(kDecodeThreads, 4) void decode_split_kernel(DecodeA
     // one value tile: the lane's probability in fixed point into the bins of its token's codes
     auto bin_tile = [&](const Tile<GH, B>& w, int k, float sv) {
         const int tile = tile0 + wave + k * NW;
+#if CQ_VIEW_KERNEL
+        // (here, where the LDS is what is waited for: among the requests of the key tiles, 4 x 131072 166 us instead of 163)
+        keep_score<VIEW>(a, (size_t)n * a.n_q_heads + hq, tile * kTileTokens + lane, sv);
+#endif
         const float p = __builtin_amdgcn_exp2f((sv - m0) + fxf);
         unsigned pf = (unsigned)(p + 0.5f);           // round to nearest
         lane_sum += pf;
@@ -655,6 +659,13 @@ __global__ __launch_bounds__(kDecodeThreads, 4) void decode_split_kernel(DecodeA
         else partial_store(part + kPartialHeader + chn, o);
     }
     if (!direct) count_and_merge();
+#if CQ_VIEW_KERNEL
+    if (direct && a.finish) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // (every wavefront's scores are written)
+        __syncthreads();
+        finish_weights<VIEW>(a, (size_t)n * a.n_q_heads + hq, t_n, tid, NT);
+    }
+#endif
 }
 #undef CQ_TILE
 #undef CQ_LAST_TILE

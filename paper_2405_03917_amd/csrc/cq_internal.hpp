@@ -141,7 +141,10 @@ struct DecodeViewArgs : DecodeArgs {
     float* weights;
     int64_t weights_stride;
     float decay;
+    bool finish;              // the last workgroup of a row adds up its weights (one query head per KV head), no second launch
 };
+// Query heads of a KV head whose weights are added up: their softmax statistics are held in LDS, 8 bytes each.
+constexpr int kMaxWeightHeads = 4096;
 
 // Tiles of a context of up to t tokens that m query tokens look at through a window with sinks (0: all of it): the
 // sinks' tiles, and the most that window + m - 1 neighbouring tokens can touch.

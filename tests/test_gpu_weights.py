@@ -108,3 +108,50 @@ def test_the_same_bits_again_and_captured():
         assert torch.equal(weights, first) and torch.equal(got, out)
         call()
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("t", [40, 3000, 9000])
+def test_one_query_head_captured(t):
+    """Without grouped queries the last workgroup of a row adds up its weights, except under capture: the same bits."""
+    cache = Cache(8, 8, 16, 16, 9024, seed=2)
+    q = queries((16, 16, 128), 1)
+    start = torch.rand(16, 16, 9024, device="cuda")
+    lens = torch.tensor([t] + [max(1, t - 37 * n) for n in range(1, 16)], dtype=torch.int32, device="cuda")
+    first, weights = start.clone(), start.clone()
+    out = cq.cq_decode_attention_weights(q, cache.k, cache.v, cache.ck, cache.cv, SCALE, cache.fmt, t, 9024, first, 0.5, lens)
+    call, got = cq.prepare_decode_attention_weights(q, cache.k, cache.v, cache.ck, cache.cv, SCALE, cache.fmt, t, 9024, weights, 0.5, seq_lens=lens)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(3):
+        weights.copy_(start)
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(weights, first) and torch.equal(got, out)
+        call()
+        torch.cuda.synchronize()
+
+
+def test_two_streams_at_once():
+    cache = Cache(8, 8, 8, 2, 4096, seed=3)
+    q = queries((2, 8, 128), 1)
+    wanted = torch.zeros(2, 8, 4096, device="cuda")
+    want = cq.cq_decode_attention_weights(q, cache.k, cache.v, cache.ck, cache.cv, SCALE, cache.fmt, 4000, 4096, wanted, 0.0)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    kept = []
+    for s in streams:
+        with torch.cuda.stream(s):
+            calls = []
+            for _ in range(8):
+                w = torch.zeros(2, 8, 4096, device="cuda")
+                call, out = cq.prepare_decode_attention_weights(q, cache.k, cache.v, cache.ck, cache.cv, SCALE, cache.fmt, 4000, 4096, w, 0.0)
+                calls.append((call, out, w))
+            kept.append(calls)
+    torch.cuda.synchronize()
+    for i in range(8):
+        for s, calls in zip(streams, kept):
+            calls[i][0](s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, want) and torch.equal(w, wanted) for calls in kept for _, out, w in calls)
