@@ -19,6 +19,8 @@ constexpr int kThreads = 256;
 constexpr int kTokensPerThread = 4;
 constexpr int kTokens = kThreads * kTokensPerThread;
 
+// AHEAD: heads whose scores are requested ahead of the statistics (one head to a KV head has no others).
+template <int AHEAD>
 __global__ __launch_bounds__(kThreads) void decode_weights_kernel(DecodeViewArgs a, int merge_wgs, int blocks)
 {
     extern __shared__ float2 stats[];                       // (M, 1 / L) per query head of the KV head
@@ -40,25 +42,33 @@ __global__ __launch_bounds__(kThreads) void decode_weights_kernel(DecodeViewArgs
     const int first = block * kTokens;
     if (first >= t_n) return;
     const size_t row0 = (size_t)n * a.n_q_heads + (size_t)hkv * qper;
+    float* acc = a.weights + (size_t)stream * a.weights_stride;
+    float old[kTokensPerThread], w[kTokensPerThread], s[AHEAD][kTokensPerThread];
+#pragma unroll
+    for (int k = 0; k < kTokensPerThread; ++k) {
+        const int tok = first + k * kThreads + tid, at = min(tok, t_n - 1);
+        old[k] = a.decay != 0.f ? acc[at] : 0.f;            // (without decay the accumulators are not read)
+#pragma unroll
+        for (int h = 0; h < AHEAD; ++h) s[h][k] = a.scores[(row0 + min(h, qper - 1)) * a.score_stride + at];
+        w[k] = 0.f;
+    }
     for (int h = wave; h < qper; h += kThreads / 64) {
         const float2 st = row_stats<false>(a, row0 + h, lane);
         if (lane == 0) stats[h] = st;
     }
     __syncthreads();
-    float* acc = a.weights + (size_t)stream * a.weights_stride;
-    float old[kTokensPerThread], w[kTokensPerThread];
+    auto add = [&](const float (&x)[kTokensPerThread], float2 st) {
 #pragma unroll
-    for (int k = 0; k < kTokensPerThread; ++k) {
-        const int tok = first + k * kThreads + tid;
-        old[k] = a.decay != 0.f && tok < t_n ? acc[tok] : 0.f;      // (without decay the accumulators are not read)
-        w[k] = 0.f;
-    }
-    for (int h = 0; h < qper; ++h) {
-        const float* s = a.scores + (row0 + h) * a.score_stride + first + tid;
-        const float2 st = stats[h];
+        for (int k = 0; k < kTokensPerThread; ++k) w[k] = __builtin_fmaf(__builtin_amdgcn_exp2f(x[k] - st.x), st.y, w[k]);
+    };
 #pragma unroll
-        for (int k = 0; k < kTokensPerThread; ++k)
-            if (first + k * kThreads + tid < t_n) w[k] = __builtin_fmaf(__builtin_amdgcn_exp2f(s[k * kThreads] - st.x), st.y, w[k]);
+    for (int h = 0; h < AHEAD; ++h)
+        if (h < qper) add(s[h], stats[h]);
+    for (int h = AHEAD; h < qper; ++h) {
+        float x[kTokensPerThread];
+#pragma unroll
+        for (int k = 0; k < kTokensPerThread; ++k) x[k] = a.scores[(row0 + h) * a.score_stride + min(first + k * kThreads + tid, t_n - 1)];
+        add(x, stats[h]);
     }
 #pragma unroll
     for (int k = 0; k < kTokensPerThread; ++k) {
@@ -76,7 +86,8 @@ cq_status launch_decode_weights(const DecodeViewArgs& a, hipStream_t stream)
     const int merge_wgs = a.n_split > 1 ? (a.batch * a.n_q_heads + 1) / 2 : 0;
     const int64_t grid = (int64_t)merge_wgs + (int64_t)a.batch * a.f.n_kv_heads * blocks;
     if (grid > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
-    hipLaunchKernelGGL(decode_weights_kernel, dim3((unsigned)grid), dim3(kThreads), sizeof(float2) * (size_t)qper, stream, a, merge_wgs, blocks);
+    hipLaunchKernelGGL(qper == 1 ? decode_weights_kernel<1> : decode_weights_kernel<4>, dim3((unsigned)grid), dim3(kThreads),
+                       sizeof(float2) * (size_t)qper, stream, a, merge_wgs, blocks);
     return hipGetLastError() == hipSuccess ? CQ_OK : CQ_ERR_HIP;
 }
 
