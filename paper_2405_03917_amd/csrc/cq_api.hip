@@ -1188,7 +1188,7 @@ size_t cq_select_workspace_bytes(int32_t batch, int32_t n_kv_heads, int32_t t)
     if (batch <= 0 || n_kv_heads <= 0 || t <= 0) return 0;
     const size_t runs = (size_t)batch * n_kv_heads * (((size_t)t + kSelectRun - 1) / kSelectRun);
     if (t <= kSelectRun) return 16;
-    return runs * (sizeof(unsigned) * (kSelectCounts + kSelectRun) + sizeof(uint4));
+    return runs * (sizeof(unsigned) * (kSelectCounts + kSelectRun) + sizeof(uint4)) + (size_t)batch * n_kv_heads * sizeof(uint2);
 }
 
 cq_status cq_select_tokens(const float* weights, int64_t weights_stride, int32_t batch, int32_t n_kv_heads, int32_t t,
@@ -1205,10 +1205,14 @@ cq_status cq_select_tokens(const float* weights, int64_t weights_stride, int32_t
         if (!workspace || !aligned16(workspace)) return CQ_ERR_INVALID_ARG;
         if (workspace_bytes < cq_select_workspace_bytes(batch, n_kv_heads, t)) return CQ_ERR_WORKSPACE_TOO_SMALL;
     }
-    unsigned* const counts = static_cast<unsigned*>(workspace);
-    unsigned* const lists = parts > 1 ? counts + (size_t)runs * kSelectCounts : nullptr;
-    const SelectArgs a{weights, weights_stride, seq_lens, batch, n_kv_heads, t, keep, n_sink, n_recent, kept, kept_lens,
-                       parts, counts, lists, parts > 1 ? reinterpret_cast<uint4*>(lists + (size_t)runs * kSelectRun) : nullptr};
+    SelectArgs a{weights, weights_stride, seq_lens, batch, n_kv_heads, t, keep, n_sink, n_recent, kept, kept_lens, parts};
+    if (parts > 1) {
+        a.counts = static_cast<unsigned*>(workspace);
+        a.lists = a.counts + (size_t)runs * kSelectCounts;
+        a.runs = reinterpret_cast<uint4*>(a.lists + (size_t)runs * kSelectRun);
+        a.found = reinterpret_cast<uint2*>(a.runs + runs);
+        a.many = parts > kSelectManyRuns || runs > kSelectAtOnce;
+    }
     return launch_select_tokens(a, static_cast<hipStream_t>(stream));
 }
 

@@ -21,7 +21,8 @@ constexpr int kDigitBits = 11;                          // three digits: 11, 11,
 constexpr int kBins = 1 << kDigitBits;
 constexpr int kPerThread = 16;                          // tokens of a run per thread, in registers
 constexpr int kPart = kSelectThreads * kPerThread;
-constexpr int kListRoom = 8192;                         // listed keys of a stream that fit in LDS (32 KB)
+constexpr int kCopies = 4;                            // of the first digits' counts in LDS, by lane
+constexpr int kListRoom = 8192;                         // listed keys of a stream that are held in LDS (32 KB)
 static_assert(kPart == kSelectRun, "as the workspace is sized");
 
 // order-preserving: larger weights have larger keys, both zeros the same; what is no number ranks below every number
@@ -149,22 +150,32 @@ __device__ __forceinline__ void clear(unsigned* hist, int tid)
     for (int i = tid; i < kBins / 4; i += NT) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
 }
-// The first digits of a run counted in LDS.  Zeros, of which there may be many (tokens that never drew weight), are counted
-// a wavefront at a time: as additions to one word they would wait for each other.
+// The first digits of a run counted in LDS, in kCopies counts of each: sign, exponent and two bits of weights that are alike
+// name a few digits, and additions to one word wait for each other.  Zeros, of which there may be many (tokens that never drew
+// weight), are counted a wavefront at a time.
 template <int NT>
 __device__ __forceinline__ void count_first_digits(const Keys<NT>& keys, unsigned* hist, int tid)
 {
     constexpr unsigned kZero = 0x80000000u;
     unsigned zeros = 0;
+    for (int i = tid; i < kBins * kCopies / 4; i += NT) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
 #pragma unroll
     for (int k = 0; k < kPerThread; ++k) {
         if (!keys.any(k)) break;
         const bool in = keys.has(k, tid), zero = in && keys.key[k] == kZero;
         zeros += (unsigned)__builtin_popcountll(__builtin_amdgcn_ballot_w64(zero));
-        if (in && !zero) atomicAdd(&hist[keys.key[k] >> 21], 1u);
+        if (in && !zero) atomicAdd(&hist[(keys.key[k] >> 21) * kCopies + (tid & (kCopies - 1))], 1u);
     }
-    if ((tid & 63) == 0 && zeros) atomicAdd(&hist[kZero >> 21], zeros);
+    if ((tid & 63) == 0 && zeros) atomicAdd(&hist[(kZero >> 21) * kCopies], zeros);
     __syncthreads();
+}
+
+__device__ __forceinline__ unsigned first_digits(const unsigned* hist, int digit)
+{
+    static_assert(kCopies == 4, "read as 16 bytes");
+    const uint4 x = reinterpret_cast<const uint4*>(hist)[digit];
+    return x.x + x.y + x.z + x.w;
 }
 
 // Positions of the run's tokens whose key is above `key`, or equals it where fewer than `need` equals lie in front, behind
@@ -217,7 +228,7 @@ __device__ __forceinline__ void write_kept(const SelectArgs& a, const Middle& m,
 template <int NT>
 __global__ __launch_bounds__(NT) void select_short_kernel(SelectArgs a)
 {
-    __shared__ __align__(16) unsigned hist[kBins];
+    __shared__ __align__(16) unsigned hist[kBins * kCopies];
     __shared__ unsigned sums[NT / 64];
     __shared__ unsigned found[2];
     const int tid = threadIdx.x, stream = blockIdx.x;
@@ -227,9 +238,14 @@ __global__ __launch_bounds__(NT) void select_short_kernel(SelectArgs a)
     keep_ends<NT>(a, m, stream, 0, 1, tid);
     if (m.len == 0) return;
     unsigned need = m.need, bin;
-    clear<NT>(hist, tid);
     count_first_digits(keys, hist, tid);
-    find_bin<NT>(hist, kBins, need, bin, sums, found, tid);
+    {
+        constexpr int N = kBins / NT;
+        unsigned c[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) c[i] = first_digits(hist, kBins - 1 - N * tid - i);
+        find_among<NT, N>(c, kBins - 1 - N * tid, need, bin, sums, found, tid);
+    }
     unsigned prefix = bin << 21, mask = (kBins - 1u) << 21;
 #pragma unroll 1
     for (int shift = 10; shift >= 0; shift -= 10) {
@@ -249,179 +265,334 @@ __global__ __launch_bounds__(NT) void select_short_kernel(SelectArgs a)
     write_kept<NT>(a, m, keys, prefix, need, 0, 0, hist, tid);
 }
 
-// Longer streams: a workgroup per run, three launches.  Each run's first digits are counted; every run then adds up the
-// stream's counts, finds the digit, and lists its keys that have it (in any order: what follows is a function of the set);
-// every run then finds the key among the stream's listed ones, and writes its own tokens.
-// (The listed keys are those of one of 2048 digits, usually less than a hundredth of the stream, and are taken to LDS.  With all
-// weights equal they are the whole stream, read from memory by each of its workgroups.)
+// Longer streams: a workgroup per run.  Each run's first digits are counted; the digit in which the key lies follows from the
+// counts of all, and every run lists its keys that have it, in any order: what follows is a function of the set; the key is found
+// among the stream's listed ones, and with it what each run has in front of its own tokens, which it then writes.  Digit and key
+// are found by every run again (three launches), or, where a stream has many, by a workgroup per stream (five).
+// (The listed keys are those of one of 2048 digits, usually less than a hundredth of the stream, and are held in LDS.  If there is
+// only one among them, such as zero for tokens that never drew weight, there is nothing to find.)
 __global__ __launch_bounds__(kSelectThreads) void select_count_kernel(SelectArgs a)
 {
-    __shared__ __align__(16) unsigned hist[kBins];
+    __shared__ __align__(16) unsigned hist[kBins * kCopies];
     const int tid = threadIdx.x, part = blockIdx.x % a.parts, stream = blockIdx.x / a.parts;
     const Middle m = middle_of(a, stream);
     Keys<kSelectThreads> keys;
     keys.load(m, part, tid);
     keep_ends<kSelectThreads>(a, m, stream, part, a.parts, tid);
     if (m.len == 0) return;
-    clear<kSelectThreads>(hist, tid);
     count_first_digits(keys, hist, tid);
-    unsigned* out = a.counts + (size_t)blockIdx.x * kBins;
-    for (int i = tid; i < kBins; i += kSelectThreads) out[i] = hist[i];
+    static_assert(kBins == 2 * kSelectCounts && kSelectRun < 65536, "two counts a word");
+    unsigned* out = a.counts + (size_t)blockIdx.x * kSelectCounts;
+    for (int i = tid; i < kSelectCounts; i += kSelectThreads) out[i] = first_digits(hist, 2 * i) | first_digits(hist, 2 * i + 1) << 16;
+}
+
+// A thread's four bins of a stream from the top (hi, hi - 1, ...), added over its runs.
+__device__ __forceinline__ void add_counts(const SelectArgs& a, int stream, int hi, unsigned (&c)[4])
+{
+    static_assert(kBins == 4 * kSelectThreads, "four bins a thread");
+    const unsigned* all = a.counts + (size_t)stream * a.parts * kSelectCounts + (hi - 3) / 2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = 0;
+#pragma unroll 1
+    for (int p0 = 0; p0 < a.parts; p0 += 8) {               // (eight runs' counts requested at once)
+        uint2 x[8];
+#pragma unroll
+        for (int p = 0; p < 8; ++p) x[p] = *reinterpret_cast<const uint2*>(all + (size_t)min(p0 + p, a.parts - 1) * kSelectCounts);
+#pragma unroll
+        for (int p = 0; p < 8; ++p) {
+            const unsigned down[4] = {x[p].y >> 16, x[p].y & 0xffffu, x[p].x >> 16, x[p].x & 0xffffu};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c[i] += p0 + p < a.parts ? down[i] : 0u;
+        }
+    }
+}
+
+// Streams of many runs: the digit, by a workgroup per stream.
+__global__ __launch_bounds__(kSelectThreads) void select_digit_kernel(SelectArgs a)
+{
+    __shared__ unsigned sums[kSelectThreads / 64];
+    __shared__ unsigned found[2];
+    const int tid = threadIdx.x, stream = blockIdx.x;
+    const Middle m = middle_of(a, stream);
+    if (m.len == 0) return;
+    unsigned c[4], need = m.need, bin;
+    add_counts(a, stream, kBins - 1 - 4 * tid, c);
+    find_among<kSelectThreads, 4>(c, kBins - 1 - 4 * tid, need, bin, sums, found, tid);
+    if (tid == 0) a.found[stream] = make_uint2(bin, need);
 }
 
 __global__ __launch_bounds__(kSelectThreads) void select_list_kernel(SelectArgs a)
 {
     __shared__ unsigned sums[kSelectThreads / 64];
     __shared__ unsigned found[2];
-    __shared__ unsigned listed;
+    __shared__ unsigned listed, lowest, highest, above;
     const int tid = threadIdx.x, part = blockIdx.x % a.parts, stream = blockIdx.x / a.parts;
+    const int lane = tid & 63;
     const Middle m = middle_of(a, stream);
     if (m.len == 0) return;
     Keys<kSelectThreads> keys;
     keys.load(m, part, tid);
-    if (tid == 0) listed = 0;
-    static_assert(kBins == 4 * kSelectThreads, "four bins a thread");
-    const int hi = kBins - 1 - 4 * tid;
-    const unsigned* all = a.counts + (size_t)stream * a.parts * kBins;
-    unsigned c[4] = {0, 0, 0, 0}, mine[4] = {0, 0, 0, 0};
-#pragma unroll 4
-    for (int p = 0; p < a.parts; ++p) {
-        const uint4 x = *reinterpret_cast<const uint4*>(all + (size_t)p * kBins + hi - 3);
-        const unsigned down[4] = {x.w, x.z, x.y, x.x};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            c[i] += down[i];
-            mine[i] = p == part ? down[i] : mine[i];
-        }
-    }
     unsigned need = m.need, bin;
-    find_among<kSelectThreads, 4>(c, hi, need, bin, sums, found, tid);
-    unsigned above;                                         // of this run, with a larger digit
-    unsigned larger = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) larger += (unsigned)(hi - i) > bin ? mine[i] : 0u;
-    block_prefix<kSelectThreads>(larger, sums, tid, &above);
-    unsigned* list = a.lists + (size_t)blockIdx.x * kPart;
-    const int lane = tid & 63;
+    if (tid == 0) {
+        listed = highest = above = 0;
+        lowest = 0xffffffffu;
+    }
+    if (a.many) {                                           // (uniform)
+        bin = a.found[stream].x;
+        __syncthreads();
+    } else {
+        unsigned c[4];
+        add_counts(a, stream, kBins - 1 - 4 * tid, c);
+        find_among<kSelectThreads, 4>(c, kBins - 1 - 4 * tid, need, bin, sums, found, tid);
+        if (part == 0 && tid == 0) a.found[stream] = make_uint2(bin, need);
+    }
+    unsigned* const list = a.lists + (size_t)blockIdx.x * kPart;
+    unsigned larger = 0, some = 0;                          // (of a wavefront: one of its listed keys)
+    bool any = false, mixed = false;
 #pragma unroll
     for (int k = 0; k < kPerThread; ++k) {
         if (!keys.any(k)) break;
-        const bool in = keys.has(k, tid) && keys.key[k] >> 21 == bin;
+        const bool has = keys.has(k, tid), in = has && keys.key[k] >> 21 == bin;
+        larger += (unsigned)__builtin_popcountll(__builtin_amdgcn_ballot_w64(has && keys.key[k] >> 21 > bin));
         const unsigned long long b = __builtin_amdgcn_ballot_w64(in);
         if (b == 0) continue;
         unsigned base = 0;
         if (lane == 0) base = atomicAdd(&listed, (unsigned)__builtin_popcountll(b));
         base = (unsigned)__builtin_amdgcn_readfirstlane((int)base);
         if (in) list[base + (unsigned)__builtin_popcountll(b & ((1ull << lane) - 1))] = keys.key[k];
+        if (!any) some = (unsigned)__builtin_amdgcn_readlane((int)keys.key[k], __builtin_ctzll(b));
+        any = true;
+        mixed = mixed || __builtin_amdgcn_ballot_w64(in && keys.key[k] != some) != 0;
+    }
+    if (lane == 0) {
+        atomicAdd(&above, larger);
+        if (any) {                                          // (of different ones any bounds will do that are not equal)
+            atomicMin(&lowest, mixed ? 0u : some);
+            atomicMax(&highest, mixed ? 0xffffffffu : some);
+        }
     }
     __syncthreads();
-    if (tid == 0) a.runs[blockIdx.x] = make_uint4(listed, above, bin, need);
+    if (tid == 0) a.runs[blockIdx.x] = make_uint4(listed, above, lowest, highest);
 }
 
+// A stream's key among the listed ones, by a workgroup.
+struct KeySearch {
+    static constexpr int kStarts = 1024, kWaves = kSelectThreads / 64;
+    struct Lds {
+        unsigned hist[kBins];
+        unsigned held[kListRoom];
+        unsigned starts[kStarts + 1];                       // where each run's keys begin among the stream's
+        unsigned sums[kWaves], found[2];
+        unsigned listed, lowest, highest;
+    };
+    Lds& s;
+    const int parts;
+    const uint4* const runs;                                // (listed, above, lowest, highest)
+    const unsigned* const lists;
+    bool in_lds, one;                                       // the listed keys are held; are all the same
+    unsigned key, need;
+
+    __device__ __forceinline__ KeySearch(Lds& lds, const SelectArgs& a, int stream)
+        : s(lds), parts(a.parts), runs(a.runs + (size_t)stream * a.parts), lists(a.lists + (size_t)stream * a.parts * kPart)
+    {
+    }
+    __device__ __forceinline__ unsigned count_of(int p) const { return parts <= kStarts ? s.starts[p + 1] - s.starts[p] : runs[p].x; }
+    // the keys of run p, by a wavefront: from memory, eight requests at a time, or held
+    template <class F>
+    __device__ __forceinline__ void of_run(int p, bool from_lds, F&& f) const
+    {
+        const int lane = threadIdx.x & 63;
+        const unsigned n = count_of(p);
+        if (from_lds) {
+            for (unsigned i = 0; i < n; i += 64) f(i + lane < n, i + lane, s.held[s.starts[p] + min(i + lane, n - 1)]);
+            return;
+        }
+        const unsigned* const l = lists + (size_t)p * kPart;
+#pragma unroll 1
+        for (unsigned i0 = 0; i0 < n; i0 += 8 * 64) {
+            unsigned x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = i0 + k * 64 < n ? l[min(i0 + k * 64 + lane, n - 1)] : 0u;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f(i0 + k * 64 + lane < n, i0 + k * 64 + lane, x[k]);
+        }
+    }
+    __device__ __forceinline__ void find(uint2 digit)
+    {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        if (wave == 0) {
+            unsigned base = 0, low = 0xffffffffu, high = 0;
+            for (int p0 = 0; p0 < parts; p0 += 64) {
+                const uint4 r = p0 + lane < parts ? runs[p0 + lane] : make_uint4(0, 0, 0xffffffffu, 0);
+                low = min(low, r.z);
+                high = max(high, r.w);
+                unsigned x = r.x;
+#pragma unroll
+                for (int d = 1; d < 64; d *= 2) {
+                    const unsigned y = __shfl_up(x, d);
+                    x += lane >= d ? y : 0u;
+                }
+                if (parts <= kStarts && p0 + lane < parts) s.starts[p0 + lane + 1] = base + x;
+                base += (unsigned)__builtin_amdgcn_readlane((int)x, 63);
+            }
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                low = min(low, (unsigned)__shfl_xor((int)low, d));
+                high = max(high, (unsigned)__shfl_xor((int)high, d));
+            }
+            if (lane == 0) {
+                s.starts[0] = 0;
+                s.listed = base;
+                s.lowest = low;
+                s.highest = high;
+            }
+        }
+        __syncthreads();
+        in_lds = parts <= kStarts && s.listed <= kListRoom;
+        one = s.lowest == s.highest;                        // (zero mostly: nothing to find)
+        key = s.lowest;
+        need = digit.y;
+        if (one) return;
+        if (in_lds && parts <= 64) {
+            for (unsigned i = tid; i < s.listed; i += kSelectThreads) {
+                int p = 0;
+#pragma unroll
+                for (int step = 32; step > 0; step >>= 1)
+                    if (p + step < parts && s.starts[p + step] <= i) p += step;
+                s.held[i] = lists[(size_t)p * kPart + (i - s.starts[p])];
+            }
+        } else if (in_lds) {
+            for (int p = wave; p < parts; p += kWaves)
+                of_run(p, false, [&](bool is, unsigned i, unsigned x) {
+                    if (is) s.held[s.starts[p] + i] = x;
+                });
+        }
+        unsigned prefix = digit.x << 21, mask = (kBins - 1u) << 21, bin;
+#pragma unroll 1
+        for (int shift = 10; shift >= 0; shift -= 10) {
+            const int bins = shift == 0 ? kBins / 2 : kBins;
+            clear<kSelectThreads>(s.hist, tid);
+            auto count = [&](bool is, unsigned, unsigned x) {
+                if (is && (x & mask) == prefix) atomicAdd(&s.hist[(x >> shift) & (bins - 1)], 1u);
+            };
+            if (in_lds) {
+                for (unsigned i = tid; i < s.listed; i += kSelectThreads) count(true, i, s.held[i]);
+            } else {
+                for (int p = wave; p < parts; p += kWaves) of_run(p, false, count);
+            }
+            __syncthreads();
+            find_bin<kSelectThreads>(s.hist, bins, need, bin, s.sums, s.found, tid);
+            prefix |= bin << shift;
+            mask |= (unsigned)(bins - 1) << shift;
+        }
+        key = prefix;
+    }
+    // of a run's tokens, those above the key and those that equal it, by a wavefront
+    __device__ __forceinline__ uint2 kept_of(int p) const
+    {
+        uint2 c = make_uint2(runs[p].y, one ? count_of(p) : 0u);
+        if (!one)
+            of_run(p, in_lds, [&](bool is, unsigned, unsigned x) {
+                c.x += (unsigned)__builtin_popcountll(__builtin_amdgcn_ballot_w64(is && x > key));
+                c.y += (unsigned)__builtin_popcountll(__builtin_amdgcn_ballot_w64(is && x == key));
+            });
+        return c;
+    }
+};
+
+// Streams of many runs: the key, and what every run's tokens have in front of them, by a workgroup per stream.
+__global__ __launch_bounds__(kSelectThreads) void select_key_kernel(SelectArgs a)
+{
+    __shared__ __align__(16) KeySearch::Lds lds;
+    const int stream = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Middle m = middle_of(a, stream);
+    if (m.len == 0) return;
+    KeySearch search(lds, a, stream);
+    search.find(a.found[stream]);
+    uint4* const runs = a.runs + (size_t)stream * a.parts;
+    for (int p = wave; p < a.parts; p += KeySearch::kWaves) {
+        const uint2 c = search.kept_of(p);
+        if (lane == 0) runs[p] = make_uint4(c.x, c.y, 0, 0);
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    unsigned gt_base = 0, eq_base = 0;
+    for (int p0 = 0; p0 < a.parts; p0 += 64) {
+        const bool is = p0 + lane < a.parts;
+        const uint4 r = is ? runs[p0 + lane] : make_uint4(0, 0, 0, 0);
+        unsigned x = r.x, y = r.y;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const unsigned gx = __shfl_up(x, d), ey = __shfl_up(y, d);
+            x += lane >= d ? gx : 0u;
+            y += lane >= d ? ey : 0u;
+        }
+        if (is) runs[p0 + lane] = make_uint4(gt_base + x - r.x, eq_base + y - r.y, search.key, search.need);
+        gt_base += (unsigned)__builtin_amdgcn_readlane((int)x, 63);
+        eq_base += (unsigned)__builtin_amdgcn_readlane((int)y, 63);
+    }
+}
+
+static_assert(kSelectManyRuns <= 64 && kSelectManyRuns <= kSelectThreads, "a thread per run in front");
+
+// The positions: MANY: behind select_key_kernel; else every run finds the key itself.
+template <bool MANY>
 __global__ __launch_bounds__(kSelectThreads) void select_write_kernel(SelectArgs a)
 {
-    __shared__ __align__(16) unsigned hist[kBins];
-    __shared__ unsigned sums[kSelectThreads / 64];
-    __shared__ unsigned found[2];
-    __shared__ unsigned held[kListRoom];
-    __shared__ unsigned starts[67];                         // of the first 64 runs; of this one; of all; the larger digits in front
+    __shared__ unsigned counts[kPerThread * kSelectThreads / 64];
     const int tid = threadIdx.x, part = blockIdx.x % a.parts, stream = blockIdx.x / a.parts;
     const Middle m = middle_of(a, stream);
     if (m.len <= part * kPart) return;
     Keys<kSelectThreads> keys;
     keys.load(m, part, tid);
-    const uint4* runs = a.runs + (size_t)stream * a.parts;
-    const unsigned* lists = a.lists + (size_t)stream * a.parts * kPart;
-    const int parts = (m.len + kPart - 1) / kPart;
-    unsigned need = runs[part].w, prefix = runs[part].z << 21, mask = (kBins - 1u) << 21, bin;
-    // where each run's listed keys begin among the stream's; what the runs in front of this one keep with a larger digit
-    if (tid < 64) {
-        unsigned base = 0, gts = 0;
-        for (int p0 = 0; p0 < parts; p0 += 64) {
-            const uint4 r = p0 + tid < parts ? runs[p0 + tid] : make_uint4(0, 0, 0, 0);
-            unsigned x = r.x;
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const unsigned y = __shfl_up(x, d);
-                x += tid >= d ? y : 0u;
+    if constexpr (MANY) {
+        const uint4 run = a.runs[blockIdx.x];
+        write_kept<kSelectThreads>(a, m, keys, run.z, run.w, run.x, run.y, counts, tid);
+    } else {
+        __shared__ __align__(16) KeySearch::Lds lds;
+        KeySearch search(lds, a, stream);
+        search.find(a.found[stream]);
+        // what the runs in front keep
+        unsigned gt = tid < part ? search.runs[tid].y : 0u, eq = 0, gt_base, eq_base;
+        if (search.one) {
+            eq = tid == 0 ? lds.starts[part] : 0u;
+        } else if (search.in_lds) {
+            for (unsigned i = tid; i < lds.starts[part]; i += kSelectThreads) {
+                gt += lds.held[i] > search.key;
+                eq += lds.held[i] == search.key;
             }
-            if (p0 == 0) starts[tid] = base + x - r.x;
-            if (part >= p0 && part < p0 + 64 && tid == part - p0) starts[64] = base + x - r.x;
-            gts += wave_sum_u32(p0 + tid < part ? r.y : 0u);
-            base += (unsigned)__builtin_amdgcn_readlane((int)x, 63);
-        }
-        if (tid == 0) {
-            starts[65] = base;
-            starts[66] = gts;
-        }
-    }
-    __syncthreads();
-    const unsigned before = starts[64], listed = starts[65], gt_runs = starts[66];
-    const bool in_lds = parts <= 64 && listed <= kListRoom;     // (uniform)
-    if (in_lds) {
-        for (unsigned i = tid; i < listed; i += kSelectThreads) {
-            int p = 0;
-            while (p + 1 < parts && starts[p + 1] <= i) ++p;
-            held[i] = lists[(size_t)p * kPart + (i - starts[p])];
-        }
-    }
-    // every listed key with its number in the stream's lists, run by run
-    auto each = [&](auto&& f) {
-        unsigned base = 0;
-        for (int p = 0; p < parts; ++p) {
-            const unsigned n = runs[p].x;
-            for (unsigned i = tid; i < n; i += kSelectThreads) f(base + i, lists[(size_t)p * kPart + i]);
-            base += n;
-        }
-    };
-    auto again = [&](auto&& f) {
-        if (in_lds) {
-            for (unsigned i = tid; i < listed; i += kSelectThreads) f(i, held[i]);
         } else {
-            each(f);
+            for (int p = tid >> 6; p < part; p += KeySearch::kWaves)
+                search.of_run(p, false, [&](bool is, unsigned, unsigned x) {
+                    gt += is && x > search.key;
+                    eq += is && x == search.key;
+                });
         }
-    };
-#pragma unroll 1
-    for (int shift = 10; shift >= 0; shift -= 10) {
-        const int bins = shift == 0 ? kBins / 2 : kBins;
-        clear<kSelectThreads>(hist, tid);
-        again([&](unsigned, unsigned key) {
-            if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (bins - 1)], 1u);
-        });
-        __syncthreads();
-        find_bin<kSelectThreads>(hist, bins, need, bin, sums, found, tid);
-        prefix |= bin << shift;
-        mask |= (unsigned)(bins - 1) << shift;
+        block_prefix<kSelectThreads>(gt, lds.sums, tid, &gt_base);
+        block_prefix<kSelectThreads>(eq, lds.sums, tid, &eq_base);
+        write_kept<kSelectThreads>(a, m, keys, search.key, search.need, gt_base, eq_base, counts, tid);
     }
-    // what the runs in front of this one keep: those above the key, and those that equal it
-    unsigned gt = 0, eq = 0, gt_base = 0, eq_base = 0;
-    if (part > 0) {                                         // (uniform)
-        again([&](unsigned i, unsigned key) {
-            gt += i < before && key > prefix;
-            eq += i < before && key == prefix;
-        });
-        block_prefix<kSelectThreads>(gt, sums, tid, &gt_base);
-        block_prefix<kSelectThreads>(eq, sums, tid, &eq_base);
-    }
-    __syncthreads();
-    write_kept<kSelectThreads>(a, m, keys, prefix, need, gt_runs + gt_base, eq_base, hist, tid);
 }
 
 // ---------------------------------------------------------------------------------- moving
 constexpr int kMoveThreads = 256;
 
 // out byte i = in byte (i + by) mod 4 W
+// (A vector, and a mask the compiler cannot see through: it makes of a choice between two words one word at a chosen index, and
+// of an array that is indexed so memory.)
 template <int W>
-__device__ __forceinline__ void rotate_bytes(unsigned (&w)[W], unsigned by)
+using Words = unsigned __attribute__((ext_vector_type(W)));
+template <int W>
+__device__ __forceinline__ void rotate_bytes(Words<W>& w, unsigned by)
 {
 #pragma unroll
     for (int d = 1; d < W; d *= 2) {
-        const bool on = (by >> 2) & (unsigned)d;
-        unsigned x[W];
+        unsigned on = 0u - ((by >> 2 & (unsigned)d) / d);
+        asm("" : "+v"(on));
+        Words<W> x;
 #pragma unroll
-        for (int i = 0; i < W; ++i) x[i] = on ? w[(i + d) % W] : w[i];
-#pragma unroll
-        for (int i = 0; i < W; ++i) w[i] = x[i];
+        for (int i = 0; i < W; ++i) x[i] = (w[(i + d) % W] & on) | (w[i] & ~on);
+        w = x;
     }
     const unsigned first = w[0];
 #pragma unroll
@@ -431,7 +602,7 @@ __device__ __forceinline__ void rotate_bytes(unsigned (&w)[W], unsigned by)
 // a token's record: Gh low bytes in 16-byte pieces, and (b = 10) the word of high bits
 template <int GH, int B>
 struct Record {
-    unsigned w[GH / 4];
+    Words<GH / 4> w;
     unsigned hi;
     __device__ __forceinline__ void load(const uint8_t* tile, int u)
     {
@@ -453,7 +624,7 @@ struct Record {
     __device__ __forceinline__ void move(int from, int to)
     {
         const unsigned by = (unsigned)(to - from) & (unsigned)(GH - 1);
-        rotate_bytes(w, by);
+        rotate_bytes<GH / 4>(w, by);
         if constexpr (B == 10) hi = __builtin_amdgcn_alignbit(hi, hi, 2 * by);
     }
 };
@@ -461,6 +632,8 @@ struct Record {
 // A wavefront moves a tile of one stream of one cache, or (tiles behind the last that is kept) clears its accumulators.
 // GATHER: from a token's old position to its new one (in the caches, or in the workspace where the caches' own places are
 // still to be read); else from the workspace to the caches.
+// Bound by the length of its chain of requests (arguments, list and lengths, codes), so each link asks for all it can: left to the
+// compiler the arguments' loads stand behind the branches that use them, a round each (2047 of 131072 tokens of 32 streams 17 us).
 template <int GH, int B, bool GATHER>
 __global__ __launch_bounds__(kMoveThreads) void move_tokens_kernel(CompactArgs a, int tiles, int work_tiles)
 {
@@ -471,30 +644,39 @@ __global__ __launch_bounds__(kMoveThreads) void move_tokens_kernel(CompactArgs a
     const int stream = blockIdx.y, which = blockIdx.z;
     const int n = stream / a.n_kv_heads, h = stream % a.n_kv_heads;
     const int r = tile * kTileTokens + lane;
-    int from = a.kept[(size_t)stream * a.keep + min(r, a.keep - 1)];       // (requested with the length)
-    const int count = min(max(a.kept_lens[n], 0), a.keep);
-    float* const weights_out = a.weights_out + (size_t)stream * a.weights_out_stride;
+    const uint8_t* const in = which ? a.in[1] : a.in[0];
+    uint8_t* const out = which ? a.out[1] : a.out[0];
+    const CacheMap map_in = a.map_in, map_out = a.map_out;
+    asm volatile("" ::"s"(in), "s"(out), "s"(map_in.block_table), "s"(map_in.bt_stride), "s"(map_in.n_pages), "s"(map_in.tiles_cap),
+                 "s"(map_in.n_kv_heads), "s"(map_out.block_table), "s"(map_out.bt_stride), "s"(map_out.n_pages), "s"(map_out.tiles_cap),
+                 "s"(map_out.n_kv_heads), "s"(a.weights), "s"(a.weights_stride), "s"(a.weights_out), "s"(a.weights_out_stride), "s"(a.kept),
+                 "s"(a.kept_lens), "s"(a.t), "s"(a.keep), "s"(a.clear_end), "s"(a.work), "s"(a.work_weights));
+    int from = a.kept[(size_t)stream * a.keep + min(r, a.keep - 1)], len = a.kept_lens[n];
+    size_t out_tile = map_out.tile_index(n, h, tile);
+    asm volatile("" : "+v"(from), "+v"(len), "+v"(out_tile));
+    const int count = min(max(len, 0), a.keep);
+    const size_t work_tile = ((size_t)stream * work_tiles + tile) * 2 + which;
+    float* const weights_out = a.weights_out + (size_t)stream * a.weights_out_stride + r;
+    float* const work_weights = a.work_weights + (size_t)stream * a.keep + r;
+    const bool weigh = which == 0 && a.weights;
     if (r < count) {
-        uint8_t* const work = a.work ? a.work + (((size_t)stream * work_tiles + tile) * 2 + which) * TILE : nullptr;
-        float* const work_weights = a.work_weights + (size_t)stream * a.keep;
         Record<GH, B> rec;
-        uint8_t* const out = work && GATHER ? work : a.out[which] + a.map_out.tile_index(n, h, tile) * TILE;
+        float w = 0.f;
         if constexpr (GATHER) {
             from = min(max(from, 0), a.t - 1);
-            rec.load(a.in[which] + a.map_in.tile_index(n, h, from / kTileTokens) * TILE, from % kTileTokens);
-            if (which == 0 && a.weights) {
-                const float x = a.weights[(size_t)stream * a.weights_stride + from];
-                if (work) work_weights[r] = x;
-                else weights_out[r] = x;
-            }
+            rec.load(in + map_in.tile_index(n, h, from / kTileTokens) * TILE, from % kTileTokens);
+            if (weigh) w = a.weights[(size_t)stream * a.weights_stride + from];
             rec.move(from % kTileTokens, lane);
+            rec.store(a.work ? a.work + work_tile * TILE : out + out_tile * TILE, lane);
+            if (weigh) *(a.work ? work_weights : weights_out) = w;
         } else {
-            rec.load(work, lane);
-            if (which == 0 && a.weights) weights_out[r] = work_weights[r];
+            rec.load(a.work + work_tile * TILE, lane);
+            if (weigh) w = *work_weights;
+            rec.store(out + out_tile * TILE, lane);
+            if (weigh) *weights_out = w;
         }
-        rec.store(out, lane);
-    } else if (which == 0 && a.weights && r < a.clear_end && (!a.work || !GATHER)) {
-        weights_out[r] = 0.f;
+    } else if (weigh && r < a.clear_end && (!a.work || !GATHER)) {
+        *weights_out = 0.f;
     }
 }
 
@@ -507,10 +689,13 @@ __global__ __launch_bounds__(kSlideThreads) void slide_tokens_kernel(CompactArgs
     constexpr int TILE = kTileTokens * GH * B / 8;
     const int tid = threadIdx.x, which = blockIdx.x & 1, stream = blockIdx.x >> 1;
     const int n = stream / a.n_kv_heads, h = stream % a.n_kv_heads;
+    uint8_t* const codes = which ? a.out[1] : a.out[0];
+    const CacheMap map = a.map_out;
+    asm volatile("" ::"s"(codes), "s"(map.block_table), "s"(map.bt_stride), "s"(map.n_pages), "s"(map.tiles_cap), "s"(map.n_kv_heads),
+                 "s"(a.weights), "s"(a.weights_out), "s"(a.weights_out_stride), "s"(a.kept), "s"(a.kept_lens), "s"(a.t), "s"(a.keep), "s"(a.clear_end));
     const int count = min(max(a.kept_lens[n], 0), a.keep);
     const int32_t* kept = a.kept + (size_t)stream * a.keep;
     const bool weigh = which == 0 && a.weights;
-    uint8_t* const codes = a.out[which];
     float* const weights = a.weights_out + (size_t)stream * a.weights_out_stride;
     auto source = [&](int r) { return r < count ? min(max(kept[r], 0), a.t - 1) : r; };
     struct Token {
@@ -521,7 +706,7 @@ __global__ __launch_bounds__(kSlideThreads) void slide_tokens_kernel(CompactArgs
     auto load = [&](Token& x, int r, int from) {
         x.from = from;
         if (from != r) {                                    // (tokens in front of the first that goes stay where they are)
-            x.rec.load(codes + a.map_out.tile_index(n, h, from / kTileTokens) * TILE, from % kTileTokens);
+            x.rec.load(codes + map.tile_index(n, h, from / kTileTokens) * TILE, from % kTileTokens);
             if (weigh) x.w = weights[from];
         }
     };
@@ -540,7 +725,7 @@ __global__ __launch_bounds__(kSlideThreads) void slide_tokens_kernel(CompactArgs
         }
         lds_barrier();                                      // the block is read
         if (moves) {
-            now.rec.store(codes + a.map_out.tile_index(n, h, r / kTileTokens) * TILE, r % kTileTokens);
+            now.rec.store(codes + map.tile_index(n, h, r / kTileTokens) * TILE, r % kTileTokens);
             if (weigh) weights[r] = now.w;
         }
         now = next;
@@ -578,8 +763,15 @@ cq_status launch_select_tokens(const SelectArgs& a, hipStream_t stream)
         hipLaunchKernelGGL(select_short_kernel<kSelectThreads>, dim3(grid), dim3(kSelectThreads), 0, stream, a);
     } else {
         hipLaunchKernelGGL(select_count_kernel, dim3(grid), dim3(kSelectThreads), 0, stream, a);
+        const unsigned streams = (unsigned)(a.batch * a.n_kv_heads);
+        if (a.many) hipLaunchKernelGGL(select_digit_kernel, dim3(streams), dim3(kSelectThreads), 0, stream, a);
         hipLaunchKernelGGL(select_list_kernel, dim3(grid), dim3(kSelectThreads), 0, stream, a);
-        hipLaunchKernelGGL(select_write_kernel, dim3(grid), dim3(kSelectThreads), 0, stream, a);
+        if (a.many) {
+            hipLaunchKernelGGL(select_key_kernel, dim3(streams), dim3(kSelectThreads), 0, stream, a);
+            hipLaunchKernelGGL(select_write_kernel<true>, dim3(grid), dim3(kSelectThreads), 0, stream, a);
+        } else {
+            hipLaunchKernelGGL(select_write_kernel<false>, dim3(grid), dim3(kSelectThreads), 0, stream, a);
+        }
     }
     return hipGetLastError() == hipSuccess ? CQ_OK : CQ_ERR_HIP;
 }

@@ -238,14 +238,21 @@ struct SelectArgs {
     int32_t* kept;            // [stream][keep]: ascending positions, -1 behind the last
     int32_t* kept_lens;       // [sequence]
     // streams of more than kSelectRun tokens: a workgroup per run of that many (`parts` of them), and in the workspace
-    // each run's counts of first digits, its listed keys, and (listed, above, digit, needed)
+    // each run's counts of first digits, its listed keys, four words about them; per stream its digit, and what is needed of it
     int parts;
+    bool many;                // digit and key of a stream by launches of their own
     unsigned* counts;
     unsigned* lists;
     uint4* runs;
+    uint2* found;
 };
 constexpr int kSelectRun = 8192;
-constexpr int kSelectCounts = 2048;
+// Digit and key of a stream by launches of their own (five instead of three) where its runs would be too many to go through, and
+// where all runs do not run at once (three workgroups a CU) and would find them again and again.  8 KV heads, weights of
+// normal logarithm, by every run -> by launches, us: 1 x 20000 22.3 -> 26.2, 4 x 131072 (512 runs) 28.1 -> 30.8, 1 x 262144 25.9 -> 30.1,
+// 4 x 262144 (1024 runs) 49.2 -> 42.4; 32 heads, 8 x 33000 (1280 runs) 61.0 -> 49.8.
+constexpr int kSelectAtOnce = 768, kSelectManyRuns = 64;
+constexpr int kSelectCounts = 1024;                     // words of a run's counts, two of 16 bits in each
 cq_status launch_select_tokens(const SelectArgs& a, hipStream_t stream);
 
 struct CompactArgs {

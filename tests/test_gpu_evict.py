@@ -76,6 +76,34 @@ def test_select_ragged_lengths_and_many_streams():
     assert np.array_equal(kept, want) and np.array_equal(new, want_new)
 
 
+@pytest.mark.parametrize("kind", ["heavy", "ties", "equal", "close", "odd", "uniform", "mostly one"])
+@pytest.mark.parametrize("batch,hkv,t,keep,n_sink,n_recent", [(1, 1, 600000, 5000, 4, 100), (3, 2, 50000, 4097, 0, 0), (100, 9, 9000, 300, 1, 7), (2, 1, 524289, 300000, 0, 9)])
+def test_select_streams_of_many_runs(kind, batch, hkv, t, keep, n_sink, n_recent):
+    """Longer than a workgroup's run, with few and many of them, at full length and ragged; weights of one value, of few, alike."""
+    rng = np.random.default_rng(t)
+    shape = (batch, hkv, t)
+    if kind == "uniform":
+        w = rng.random(shape, dtype=np.float32)
+    elif kind == "mostly one":                              # with neighbours of the same first digits
+        w = np.where(rng.random(shape) < 0.99, np.float32(0.3), rng.random(shape, dtype=np.float32) * np.float32(0.05) + np.float32(0.27))
+    else:
+        w = _weights(kind, shape, rng)
+    lens = [t] + [int(x) for x in rng.integers(0, t, batch - 1)]
+    kept, new = _select(w, t, keep, n_sink, n_recent, lens)
+    want, want_new = select_oracle(w, t, lens, keep, n_sink, n_recent)
+    assert np.array_equal(kept, want) and np.array_equal(new, want_new)
+    again = _select(w, t, keep, n_sink, n_recent, lens)
+    assert np.array_equal(again[0], kept)
+
+
+def test_select_from_eight_million():
+    t, keep = 8500000, 2000
+    for w in (np.random.default_rng(1).random((1, 1, t), dtype=np.float32) ** 8, np.zeros((1, 1, t), dtype=np.float32)):
+        kept, new = _select(w, t, keep, 4, 32)
+        want, want_new = select_oracle(w, t, [t], keep, 4, 32)
+        assert np.array_equal(kept, want) and np.array_equal(new, want_new)
+
+
 def _moved(cache, which, kept, new, old):
     """Codes [B, t_cap_out, G] of a cache after the move, given those it held before."""
     f = cache.fmt
