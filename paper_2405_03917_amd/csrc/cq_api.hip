@@ -1269,11 +1269,13 @@ cq_status compact_common(const void* k_codes, const void* v_codes, const float* 
     if (!pages && (same_k || same_v) && t_cap_out != t_cap) return CQ_ERR_INVALID_ARG;
     if (weights && (same_w ? weights_out_stride != weights_stride : overlap(weights_out, wo_bytes, weights, w_bytes))) return CQ_ERR_INVALID_ARG;
     const bool in_place = same_k || same_v || same_w;
-    // Streams that fill the CUs move their tokens forward themselves, in one launch; fewer go through the workspace, where
-    // all CUs take part.
+    // In place, place by place: a workgroup per stream moves its tokens forward, in one launch; long lists of few streams go through
+    // the workspace, where all CUs take part.  Streams x tokens that stay, one workgroup a stream -> workspace, us: CQ-8c8b 8 x 4096
+    // 8.0 -> 10.5, 8 x 8192 13.2 -> 10.5, 32 x 16384 27.1 -> 17.1, 128 x 16384 33.9 -> 52.0, 128 x 65536 180 -> 227; CQ-4c8b 8 x 4096
+    // 8.3 -> 10.3, 32 x 8192 22.8 -> 19.1, 128 x 65536 242 -> 529; CQ-2c8b 8 x 4096 10.2 -> 10.4, 128 x 65536 459 -> 860.
     const bool same_places = !pages || (pages->block_table == pages_out->block_table && pages->row_stride == pages_out->row_stride &&
                                         pages->n_pages == pages_out->n_pages);
-    a.slide = same_k && same_v && (!weights || same_w) && same_places && 2 * streams >= 256;
+    a.slide = same_k && same_v && (!weights || same_w) && same_places && (keep <= 4096 || 2 * streams >= 256);
     const size_t codes = round256(compact_codes_bytes(f, batch, keep));
     a.work = nullptr;
     a.work_weights = nullptr;

@@ -224,6 +224,19 @@ def test_sub_byte_formats_move_as_their_fused_format():
     assert torch.equal(k, cache.k) and torch.equal(v, cache.v)
 
 
+@pytest.mark.parametrize("c,b", FORMATS)
+@pytest.mark.parametrize("batch,hkv,keep", [(1, 2, 4500), (2, 64, 4500), (1, 1, 4096)])
+def test_long_lists_in_place_equal_those_moved_elsewhere(c, b, batch, hkv, keep):
+    t, cap = 5001, 5056
+    cache = Cache(c, b, hkv, batch, cap, seed=keep)
+    weights = torch.rand(batch, hkv, cap, device="cuda")
+    kept, lens = cq.cq_select_tokens(weights, t, keep, 3, 100, torch.tensor([t] + [4700] * (batch - 1), dtype=torch.int32, device="cuda"))
+    k, v, w = cache.k.clone(), cache.v.clone(), weights.clone()
+    cq.cq_compact_cache(cache.k, cache.v, weights, cache.fmt, kept, lens, t, cap, k, v, w, cap)
+    cq.cq_compact_cache(cache.k, cache.v, weights, cache.fmt, kept, lens, t, cap)
+    assert torch.equal(cache.k, k) and torch.equal(cache.v, v) and torch.equal(weights, w)
+
+
 def test_captured():
     cache = Cache(4, 8, 4, 4, 1024, seed=8)
     f = cache.fmt
