@@ -9,7 +9,7 @@
 // splits too (the attention kernel does both itself where one query head's context is short: launch_decode_view).  Every sum is
 // formed by one thread in a fixed order: no atomics, equal calls give equal bits.
 // Bound by memory: 4 bytes a query head and token (the scores, mostly still in the caches) and 8 a KV head and token.  Of
-// 4 x 131072 tokens, 32 heads: 47 us for 67 MB of scores and 134 of accumulators.  Tokens per thread 4: 8 or 16 are slower.
+// 4 x 131072 tokens, 32 heads: 37 us for 67 MB of scores and 134 of accumulators (5.4 TB/s).  Tokens per thread 4: 8 or 16 are slower.
 #include "cq_decode_split.hpp"
 
 namespace cq {
@@ -19,8 +19,6 @@ constexpr int kThreads = 256;
 constexpr int kTokensPerThread = 4;
 constexpr int kTokens = kThreads * kTokensPerThread;
 
-// AHEAD: heads whose scores are requested ahead of the statistics (one head to a KV head has no others).
-template <int AHEAD>
 __global__ __launch_bounds__(kThreads) void decode_weights_kernel(DecodeViewArgs a, int merge_wgs, int blocks)
 {
     extern __shared__ float2 stats[];                       // (M, 1 / L) per query head of the KV head
@@ -43,32 +41,28 @@ __global__ __launch_bounds__(kThreads) void decode_weights_kernel(DecodeViewArgs
     if (first >= t_n) return;
     const size_t row0 = (size_t)n * a.n_q_heads + (size_t)hkv * qper;
     float* acc = a.weights + (size_t)stream * a.weights_stride;
-    float old[kTokensPerThread], w[kTokensPerThread], s[AHEAD][kTokensPerThread];
+    // The accumulators and the first head's scores are requested ahead of the statistics (of four heads all at once: no faster).
+    float old[kTokensPerThread], w[kTokensPerThread], x[kTokensPerThread];
+    auto request = [&](int h) {
+#pragma unroll
+        for (int k = 0; k < kTokensPerThread; ++k) x[k] = a.scores[(row0 + h) * a.score_stride + min(first + k * kThreads + tid, t_n - 1)];
+    };
 #pragma unroll
     for (int k = 0; k < kTokensPerThread; ++k) {
-        const int tok = first + k * kThreads + tid, at = min(tok, t_n - 1);
-        old[k] = a.decay != 0.f ? acc[at] : 0.f;            // (without decay the accumulators are not read)
-#pragma unroll
-        for (int h = 0; h < AHEAD; ++h) s[h][k] = a.scores[(row0 + min(h, qper - 1)) * a.score_stride + at];
+        old[k] = a.decay != 0.f ? acc[min(first + k * kThreads + tid, t_n - 1)] : 0.f;      // (without decay the accumulators are not read)
         w[k] = 0.f;
     }
+    request(0);
     for (int h = wave; h < qper; h += kThreads / 64) {
         const float2 st = row_stats<false>(a, row0 + h, lane);
         if (lane == 0) stats[h] = st;
     }
     __syncthreads();
-    auto add = [&](const float (&x)[kTokensPerThread], float2 st) {
+    for (int h = 0; h < qper; ++h) {
+        const float2 st = stats[h];
 #pragma unroll
         for (int k = 0; k < kTokensPerThread; ++k) w[k] = __builtin_fmaf(__builtin_amdgcn_exp2f(x[k] - st.x), st.y, w[k]);
-    };
-#pragma unroll
-    for (int h = 0; h < AHEAD; ++h)
-        if (h < qper) add(s[h], stats[h]);
-    for (int h = AHEAD; h < qper; ++h) {
-        float x[kTokensPerThread];
-#pragma unroll
-        for (int k = 0; k < kTokensPerThread; ++k) x[k] = a.scores[(row0 + h) * a.score_stride + min(first + k * kThreads + tid, t_n - 1)];
-        add(x, stats[h]);
+        if (h + 1 < qper) request(h + 1);
     }
 #pragma unroll
     for (int k = 0; k < kTokensPerThread; ++k) {
@@ -86,8 +80,7 @@ cq_status launch_decode_weights(const DecodeViewArgs& a, hipStream_t stream)
     const int merge_wgs = a.n_split > 1 ? (a.batch * a.n_q_heads + 1) / 2 : 0;
     const int64_t grid = (int64_t)merge_wgs + (int64_t)a.batch * a.f.n_kv_heads * blocks;
     if (grid > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
-    hipLaunchKernelGGL(qper == 1 ? decode_weights_kernel<1> : decode_weights_kernel<4>, dim3((unsigned)grid), dim3(kThreads),
-                       sizeof(float2) * (size_t)qper, stream, a, merge_wgs, blocks);
+    hipLaunchKernelGGL(decode_weights_kernel, dim3((unsigned)grid), dim3(kThreads), sizeof(float2) * (size_t)qper, stream, a, merge_wgs, blocks);
     return hipGetLastError() == hipSuccess ? CQ_OK : CQ_ERR_HIP;
 }
 
