@@ -402,10 +402,10 @@ cq_status launch_decode_view(const DecodeViewArgs& a_in, hipStream_t stream)
     if (decode_takes_quads(a_in, view_tiles(a_in.t, 1, a_in.window, a_in.n_sink), &a)) return launch_decode_quad_view(a, stream);
     // With the scores kept, the weights need all splits of a row and all query heads of a KV head.  One query head and a short
     // context, or one of medium length where other rows' workgroups run meanwhile: the row's last workgroup adds them up as it merges
-    // the output.  Otherwise a kernel of its own, which merges too.  32 heads, a kernel of its own -> here, us:
-    // CQ-8c8b 1 x 100 11.5 -> 8.0, 1 x 2000 12.5 -> 10.8, 1 x 4096 12.9 -> 11.5, 1 x 8192 13.5 -> 14.7, 1 x 16384 17.2 -> 23.1, 8 x 2000 15.6 ->
-    // 12.3, 8 x 16384 45.2 -> 40.8, 32 x 4096 46.9 -> 43.2; CQ-4c8b 8 x 4096 23.8 -> 21.7; CQ-2c8b 1 x 1000 16.0 -> 14.0, 8 x 8192 61.5 -> 61.2;
-    // CQ-8c10b 1 x 1000 18.8 -> 15.7, 8 x 8192 41.2 -> 41.4.
+    // the output.  Otherwise a kernel of its own, which merges too.  32 heads, a kernel of its own -> here, us (in launches back to back):
+    // CQ-8c8b 1 x 100 9.8 -> 7.3, 1 x 2000 9.9 -> 9.8, 1 x 4096 10.4 -> 10.7, 1 x 16384 12.9 -> 12.9 (there the kernel), 8 x 2000 12.6 ->
+    // 10.6, 8 x 8192 25.5 -> 22.7, 8 x 16384 42.5 -> 40.7, 32 x 4096 44.6 -> 43.4; CQ-4c8b 8 x 4096 21.6 -> 19.6; CQ-2c8b 1 x 1000 14.4 -> 13.1,
+    // 8 x 8192 58.8 -> 59.2; CQ-8c10b 1 x 1000 13.1 -> 11.8, 8 x 8192 39.4 -> 41.2.
     const int rows = a.batch * a.n_q_heads;
     const bool short_rows = a.scores && a.n_q_heads == a.f.n_kv_heads && (a.t <= 4096 || (a.t <= 16384 && rows >= 256));
     a.merge_counters = a.n_split > 1 && (!a.scores || short_rows) ? g_merge_counters.for_stream(stream, a.batch * a.n_q_heads) : nullptr;
