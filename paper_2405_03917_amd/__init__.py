@@ -1091,6 +1091,24 @@ def cq_probe_mfma(a, b, stream=None):
 
 # ---------------------------------------------------------------- caches that stay bounded
 
+def _on_stream(stream, prepare, *args, **kwargs) -> tuple:
+    """Prepare a call and make it on `stream`, whose memory pool what is allocated for it comes from: work on the current stream
+    that still uses memory freed there is not in its way, nor is what is allocated there next.  Returns the outputs."""
+    import torch
+    if stream is None:
+        made = prepare(*args, **kwargs)
+    else:
+        user = torch.cuda.current_stream()
+        with torch.cuda.stream(stream):
+            made = prepare(*args, **kwargs)
+    call, outs = (made, ()) if isinstance(made, PreparedCall) else (made[0], tuple(made[1:]))
+    call(stream)
+    if stream is not None:
+        for out in outs:
+            out.record_stream(user)
+    return outs
+
+
 def _same_device(*tensors) -> None:
     """All on the current device (the library launches there, on a stream of that device)."""
     import torch
@@ -1212,20 +1230,16 @@ def cq_decode_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, sc
                                window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None,
                                stream=None):
     """cq_decode_attention through a sliding window: the last `window` tokens of each sequence and its first `n_sink`."""
-    call, out = prepare_decode_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t, t_cap, window, n_sink,
-                                                None, seq_lens, tokens_per_split, out, workspace)
-    call(stream)
-    return out
+    return _on_stream(stream, prepare_decode_attention_window, q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t,
+                      t_cap, window, n_sink, None, seq_lens, tokens_per_split, out, workspace)[0]
 
 
 def cq_decode_attention_window_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
                                      pages: PageTable, window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0,
                                      out=None, workspace=None, stream=None):
     """cq_decode_attention_window over paged pools (pages outside the window and the sinks are not looked at)."""
-    call, out = prepare_decode_attention_window(q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0, window, n_sink,
-                                                pages, seq_lens, tokens_per_split, out, workspace)
-    call(stream)
-    return out
+    return _on_stream(stream, prepare_decode_attention_window, q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0,
+                      window, n_sink, pages, seq_lens, tokens_per_split, out, workspace)[0]
 
 
 def cq_decode_step_window(q, x_k_new, x_v_new, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
@@ -1234,10 +1248,8 @@ def cq_decode_step_window(q, x_k_new, x_v_new, k_codes, v_codes, k_centroids, v_
     """cq_decode_step through a sliding window with sinks: the new token is encoded at position t - 1 (seq_lens[n] - 1)."""
     if x_k_new is None or x_v_new is None:
         raise TypeError("x_k_new and x_v_new must be CUDA/HIP tensors")
-    call, out = prepare_decode_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t, t_cap, window, n_sink,
-                                                None, seq_lens, tokens_per_split, out, workspace, x_k_new, x_v_new)
-    call(stream)
-    return out
+    return _on_stream(stream, prepare_decode_attention_window, q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t,
+                      t_cap, window, n_sink, None, seq_lens, tokens_per_split, out, workspace, x_k_new, x_v_new)[0]
 
 
 def cq_decode_step_window_paged(q, x_k_new, x_v_new, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
@@ -1246,10 +1258,8 @@ def cq_decode_step_window_paged(q, x_k_new, x_v_new, k_pool, v_pool, k_centroids
     """cq_decode_step_window over paged pools."""
     if x_k_new is None or x_v_new is None:
         raise TypeError("x_k_new and x_v_new must be CUDA/HIP tensors")
-    call, out = prepare_decode_attention_window(q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0, window, n_sink,
-                                                pages, seq_lens, tokens_per_split, out, workspace, x_k_new, x_v_new)
-    call(stream)
-    return out
+    return _on_stream(stream, prepare_decode_attention_window, q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0,
+                      window, n_sink, pages, seq_lens, tokens_per_split, out, workspace, x_k_new, x_v_new)[0]
 
 
 def cq_chunk_window_workspace_bytes(fmt: CQFormat, batch: int, n_q_heads: int, m: int, t: int, window: int, n_sink: int = 0,
@@ -1287,20 +1297,16 @@ def cq_chunk_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, sca
                               stream=None):
     """cq_chunk_attention through sliding windows: each of the last m tokens sees the `window` tokens up to its own position
     and the sequence's first `n_sink`."""
-    call, out = prepare_chunk_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t, t_cap, window, n_sink,
-                                               None, seq_lens, tokens_per_split, out, workspace)
-    call(stream)
-    return out
+    return _on_stream(stream, prepare_chunk_attention_window, q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t, t_cap,
+                      window, n_sink, None, seq_lens, tokens_per_split, out, workspace)[0]
 
 
 def cq_chunk_attention_window_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
                                     pages: PageTable, window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0,
                                     out=None, workspace=None, stream=None):
     """cq_chunk_attention_window over paged pools."""
-    call, out = prepare_chunk_attention_window(q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0, window, n_sink,
-                                               pages, seq_lens, tokens_per_split, out, workspace)
-    call(stream)
-    return out
+    return _on_stream(stream, prepare_chunk_attention_window, q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0,
+                      window, n_sink, pages, seq_lens, tokens_per_split, out, workspace)[0]
 
 
 def cq_decode_weights_workspace_bytes(fmt: CQFormat, batch: int, n_q_heads: int, t: int, tokens_per_split: int = 0) -> int:
@@ -1330,20 +1336,16 @@ def cq_decode_attention_weights(q, k_codes, v_codes, k_centroids, v_centroids, s
                                 stream=None):
     """cq_decode_attention that also adds each cached token's attention weight, summed over the query heads of its KV head, to
     `weights` fp32 [B, n_kv_heads, tokens]: weights = decay weights + this step's (decay 0: weights are not read)."""
-    call, out = prepare_decode_attention_weights(q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t, t_cap, weights, decay,
-                                                 None, seq_lens, tokens_per_split, out, workspace)
-    call(stream)
-    return out
+    return _on_stream(stream, prepare_decode_attention_weights, q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t,
+                      t_cap, weights, decay, None, seq_lens, tokens_per_split, out, workspace)[0]
 
 
 def cq_decode_attention_weights_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
                                       pages: PageTable, weights, decay: float = 1.0, seq_lens=None, tokens_per_split: int = 0,
                                       out=None, workspace=None, stream=None):
     """cq_decode_attention_weights over paged pools."""
-    call, out = prepare_decode_attention_weights(q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0, weights, decay,
-                                                 pages, seq_lens, tokens_per_split, out, workspace)
-    call(stream)
-    return out
+    return _on_stream(stream, prepare_decode_attention_weights, q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0,
+                      weights, decay, pages, seq_lens, tokens_per_split, out, workspace)[0]
 
 
 def cq_chunk_weights_workspace_bytes(fmt: CQFormat, batch: int, n_q_heads: int, m: int, t: int) -> int:
@@ -1376,13 +1378,15 @@ def cq_chunk_weights(q, k_codes, k_centroids, scale: float, fmt: CQFormat, t: in
                      seq_lens=None, workspace=None, stream=None) -> None:
     """weights fp32 [B, n_kv_heads, tokens] = decay weights + the causal attention weights of the last m tokens of each sequence,
     summed over them and over the query heads of each KV head; q fp16 [B, m, Hq, head_dim]."""
-    prepare_chunk_weights(q, k_codes, k_centroids, scale, fmt, t, t_cap, weights, decay, None, seq_lens, workspace)(stream)
+    _on_stream(stream, prepare_chunk_weights, q, k_codes, k_centroids, scale, fmt, t, t_cap, weights, decay, None, seq_lens,
+               workspace)
 
 
 def cq_chunk_weights_paged(q, k_pool, k_centroids, scale: float, fmt: CQFormat, t: int, pages: PageTable, weights, decay: float = 1.0,
                            seq_lens=None, workspace=None, stream=None) -> None:
     """cq_chunk_weights over a paged key pool."""
-    prepare_chunk_weights(q, k_pool, k_centroids, scale, fmt, t, 0, weights, decay, pages, seq_lens, workspace)(stream)
+    _on_stream(stream, prepare_chunk_weights, q, k_pool, k_centroids, scale, fmt, t, 0, weights, decay, pages, seq_lens,
+               workspace)
 
 
 def cq_select_workspace_bytes(batch: int, n_kv_heads: int, t: int) -> int:
@@ -1420,9 +1424,7 @@ def cq_select_tokens(weights, t: int, keep: int, n_sink: int = 0, n_recent: int 
     """The `keep` tokens that stay of every sequence and KV head: its first n_sink, its last n_recent, and the heaviest by
     `weights` fp32 [B, n_kv_heads, tokens].  Returns (kept int32 [B, n_kv_heads, keep], ascending, -1 behind the last; kept_lens
     int32 [B], the sequences' new lengths)."""
-    call, kept, kept_lens = prepare_select_tokens(weights, t, keep, n_sink, n_recent, seq_lens, kept, kept_lens, workspace)
-    call(stream)
-    return kept, kept_lens
+    return _on_stream(stream, prepare_select_tokens, weights, t, keep, n_sink, n_recent, seq_lens, kept, kept_lens, workspace)
 
 
 def cq_compact_workspace_bytes(fmt: CQFormat, batch: int, keep: int) -> int:
@@ -1475,12 +1477,12 @@ def cq_compact_cache(k_codes, v_codes, weights, fmt: CQFormat, kept, kept_lens, 
                      weights_out=None, t_cap_out=None, workspace=None, stream=None) -> None:
     """Move the tokens `kept` (cq_select_tokens) of every sequence and KV head, codes and accumulators (weights None: codes
     alone), to positions 0, 1, ...: in place, or into k_out, v_out, weights_out of capacity t_cap_out."""
-    prepare_compact_cache(k_codes, v_codes, weights, fmt, kept, kept_lens, t, t_cap, k_out, v_out, weights_out, t_cap_out,
-                          workspace=workspace)(stream)
+    _on_stream(stream, prepare_compact_cache, k_codes, v_codes, weights, fmt, kept, kept_lens, t, t_cap, k_out, v_out,
+               weights_out, t_cap_out, workspace=workspace)
 
 
 def cq_compact_cache_paged(k_pool, v_pool, weights, fmt: CQFormat, kept, kept_lens, t: int, pages: PageTable, k_pool_out=None,
                            v_pool_out=None, weights_out=None, pages_out=None, workspace=None, stream=None) -> None:
     """cq_compact_cache from the pages of `pages` to those of `pages_out` (default: in place)."""
-    prepare_compact_cache(k_pool, v_pool, weights, fmt, kept, kept_lens, t, 0, k_pool_out, v_pool_out, weights_out, 0, pages, pages_out,
-                          workspace)(stream)
+    _on_stream(stream, prepare_compact_cache, k_pool, v_pool, weights, fmt, kept, kept_lens, t, 0, k_pool_out, v_pool_out,
+               weights_out, 0, pages, pages_out, workspace)

@@ -265,6 +265,36 @@ def test_captured():
         torch.cuda.synchronize()
 
 
+def test_what_a_call_on_another_stream_allocates_is_its_own():
+    """Workspaces and outputs of a call on a stream, while the current stream fills freed memory of the same sizes."""
+    cache = Cache(8, 8, 8, 2, 4096, seed=9)
+    q, rows = queries((2, 8, 128), 1), queries((2, 5, 8, 128), 2)
+    drawn = torch.rand(2, 8, 20000, device="cuda")
+    side = torch.cuda.Stream()
+
+    def all_of_them(stream):
+        w, chunk = torch.zeros(2, 8, 4096, device="cuda"), torch.zeros(2, 8, 4096, device="cuda")
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+        args = (cache.k, cache.v, cache.ck, cache.cv, SCALE, cache.fmt, 4000, 4096)
+        out = [cq.cq_decode_attention_window(q, *args, 3000, 5, stream=stream), cq.cq_decode_attention_weights(q, *args, w, stream=stream),
+               cq.cq_chunk_attention_window(rows, *args, 3000, 5, stream=stream), *cq.cq_select_tokens(drawn, 20000, 500, 4, 32, stream=stream)]
+        cq.cq_chunk_weights(rows, cache.k, cache.ck, SCALE, cache.fmt, 4000, 4096, chunk, stream=stream)
+        return out + [w, chunk]
+
+    want = all_of_them(None)
+    torch.cuda.synchronize()
+    sizes = [1 << k for k in range(9, 23)]
+    for _ in range(10):
+        held = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+        del held
+        got = all_of_them(side)
+        for n in sizes:
+            torch.empty(n, dtype=torch.uint8, device="cuda").fill_(255)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
 @pytest.mark.parametrize("c,b", FORMATS)
 def test_a_bounded_cache_in_use(c, b):
     """Prompt, weights over some steps, eviction, more steps with the accumulators carried on, a second eviction, and a window
