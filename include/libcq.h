@@ -504,6 +504,8 @@ CQ_API cq_status cq_chunk_attention_rope_paged(const void *q, const void *k_pool
 /*
  * Caches that stay bounded.  A sequence that goes on and on either looks at its cache through a window (the first two
  * groups of calls below), or keeps the tokens that attention weighs most and drops the others (the last two).
+ * A workspace belongs to one call at a time: calls that may overlap (on several streams, in graphs that are replayed at once)
+ * need one each.
  *
  * cq_decode_attention_window[_paged] -- cq_decode_attention[_paged] through a sliding window with sinks: the query, at
  * position p = t - 1 (seq_lens[n] - 1), attends to the tokens i <= p with i > p - window or i < n_sink.

@@ -180,6 +180,12 @@ __device__ __forceinline__ unsigned first_digits(const unsigned* hist, int digit
     return x.x + x.y + x.z + x.w;
 }
 
+// `from` and the lanes in front of this one that are in the mask
+__device__ __forceinline__ unsigned lanes_below(unsigned long long mask, unsigned from)
+{
+    return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, from));
+}
+
 // Positions of the run's tokens whose key is above `key`, or equals it where fewer than `need` equals lie in front, behind
 // gt_base, eq_base such tokens of earlier runs.
 template <int NT>
@@ -188,7 +194,6 @@ __device__ __forceinline__ void write_kept(const SelectArgs& a, const Middle& m,
 {
     constexpr int kWaves = NT / 64, N = kPerThread * kWaves / 64;      // counts per lane of a wavefront
     const int lane = tid & 63, wave = tid >> 6;
-    const unsigned long long below = (1ull << lane) - 1;
 #pragma unroll
     for (int k = 0; k < kPerThread; ++k) {
         const bool in = keys.has(k, tid);
@@ -220,8 +225,7 @@ __device__ __forceinline__ void write_kept(const SelectArgs& a, const Middle& m,
         const bool in = keys.has(k, tid), gt = in && keys.key[k] > key, eq = in && keys.key[k] == key;
         const unsigned long long gts = __builtin_amdgcn_ballot_w64(gt), eqs = __builtin_amdgcn_ballot_w64(eq);
         const unsigned at = counts[k * kWaves + wave];
-        const unsigned g = gt_base + (at & 0xffffu) + (unsigned)__builtin_popcountll(gts & below);
-        const unsigned e = eq_base + (at >> 16) + (unsigned)__builtin_popcountll(eqs & below);
+        const unsigned g = lanes_below(gts, gt_base + (at & 0xffffu)), e = lanes_below(eqs, eq_base + (at >> 16));
         if (gt || (eq && e < need)) m.kept[a.n_sink + g + min(e, need)] = a.n_sink + keys.first + k * NT + tid;
     }
 }
@@ -361,7 +365,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_list_kernel(SelectArgs 
         unsigned base = 0;
         if (lane == 0) base = atomicAdd(&listed, (unsigned)__builtin_popcountll(b));
         base = (unsigned)__builtin_amdgcn_readfirstlane((int)base);
-        if (in) list[base + (unsigned)__builtin_popcountll(b & ((1ull << lane) - 1))] = keys.key[k];
+        if (in) list[lanes_below(b, base)] = keys.key[k];
         if (!any) some = (unsigned)__builtin_amdgcn_readlane((int)keys.key[k], __builtin_ctzll(b));
         any = true;
         mixed = mixed || __builtin_amdgcn_ballot_w64(in && keys.key[k] != some) != 0;
