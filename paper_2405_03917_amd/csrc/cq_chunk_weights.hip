@@ -11,7 +11,7 @@
 // 256 query rows in LDS; a wavefront takes 64-token tiles by itself, gathers their keys from the codebook straight into the
 // operand of S^T = K Q^T (v_mfma_f32_32x32x16_f16: a lane's 8 channels are the centroids of its token's codes) and keeps
 // them for all row blocks.  Every sum has a fixed order: equal calls give equal bits.
-// Bound by the vector ALU, busy 0.80 of the time: of 1.06 M clocks of a pass over 4 x 32768 tokens of CQ-4c8b with 500 query tokens,
+// Bound by the vector ALU, busy 0.72 to 0.80 of the time: of 1.07 M clocks of a pass over 4 x 32768 tokens of CQ-4c8b with 500 query tokens,
 // 32 / 8 heads, the products take 0.52 M, an exponential per score at a quarter of the vector rate 0.51 M, a fused multiply-add before and
 // one behind it 0.26 M, and they overlap in part: 1.17 ms for both passes, 913 TFLOP/s.  Short calls are two launches of 11 us each, the codebook's way to LDS among them.
 #include <type_traits>
