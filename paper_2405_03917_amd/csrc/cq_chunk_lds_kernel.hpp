@@ -2,6 +2,7 @@
 // kernels: as a function that both inline, the first was scheduled otherwise.)
 #if CQ_VIEW_KERNEL
 #define CQ_TILE(i) it.seen.tile(i)
+#define CQ_REQUESTED(i) it.seen.requested(i, it.tile0, it.tile1)
 #define CQ_HIDES(tile) (CQ_TILE(tile) * kTileTokens + kTileTokens - 1 > it.pos_first || before_window(a, CQ_TILE(tile), it.pos_last))
 #define CQ_SEES(tok) in_window(a, tok, it.pos)
 template <int C, bool HALF>
@@ -9,6 +10,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kWaves *
 {
 #else
 #define CQ_TILE(i) (i)
+#define CQ_REQUESTED(i) max(min(i, it.tile1 - 1), it.tile0)
 #define CQ_HIDES(tile) tile * kTileTokens + kTileTokens - 1 > it.pos_first
 #define CQ_SEES(tok) tok <= it.pos
 template <int C, bool HALF>
@@ -65,7 +67,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kWaves *
     u32x4 rk[4][PL], rv[4][PL];                             // token 16 i + col, token 16 i + vtok
     unsigned zk[4][GH / 16], zv[4][2];
     auto request = [&](const Item& it, int tile) {
-        const size_t at = a.map.tile_index(it.n, hkv, CQ_TILE(max(min(tile, it.tile1 - 1), it.tile0))) * TILE_BYTES;
+        const size_t at = a.map.tile_index(it.n, hkv, CQ_REQUESTED(tile)) * TILE_BYTES;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -395,5 +397,6 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kWaves *
     }
 }
 #undef CQ_TILE
+#undef CQ_REQUESTED
 #undef CQ_HIDES
 #undef CQ_SEES

@@ -36,7 +36,7 @@ template <>
 struct Seen<kWindow> {
     int n_tiles, head, skip, first, n_sink;             // first: the window's first token
     __device__ __forceinline__ Seen() = default;
-    __device__ __forceinline__ Seen(const DecodeViewArgs& a, int t_n)
+    __host__ __device__ __forceinline__ Seen(const DecodeViewArgs& a, int t_n)
     {
         n_sink = a.n_sink;
         first = max(0, t_n - a.window);
@@ -45,9 +45,9 @@ struct Seen<kWindow> {
         skip = at - head;
         n_tiles = (t_n + kTileTokens - 1) / kTileTokens - skip;
     }
-    __device__ __forceinline__ int tile(int i) const { return i < head ? i : i + skip; }
-    __device__ __forceinline__ bool edge(int i) const { return i == n_tiles - 1 || i == head || i == head - 1; }
-    __device__ __forceinline__ bool token(int tok, int t_n) const { return tok < t_n && (tok >= first || tok < n_sink); }
+    __host__ __device__ __forceinline__ int tile(int i) const { return i < head ? i : i + skip; }
+    __host__ __device__ __forceinline__ bool edge(int i) const { return i == n_tiles - 1 || i == head || i == head - 1; }
+    __host__ __device__ __forceinline__ bool token(int tok, int t_n) const { return tok < t_n && (tok >= first || tok < n_sink); }
 };
 
 // LayerPtrs as the kernel reads it.  A pointer read from memory could point anywhere (LDS,

@@ -100,21 +100,24 @@ __device__ __forceinline__ unsigned entry(unsigned z, int k, unsigned base)
 struct ChunkSeen {
     int n_tiles, head, skip;
     __device__ __forceinline__ ChunkSeen() = default;
-    __device__ __forceinline__ ChunkSeen(const ChunkViewArgs& a, int first, int last)
+    __host__ __device__ __forceinline__ ChunkSeen(const ChunkViewArgs& a, int first, int last)
     {
         const int at = max(0, first - a.window + 1) / kTileTokens;
         head = min((a.n_sink + kTileTokens - 1) / kTileTokens, at);
         skip = at - head;
         n_tiles = last / kTileTokens + 1 - skip;
     }
-    __device__ __forceinline__ int tile(int i) const { return i < head ? i : i + skip; }
+    __host__ __device__ __forceinline__ int tile(int i) const { return i < head ? i : i + skip; }
+    // The tile requested for place i of a walk over places tile0 .. tile1 - 1: behind its end the last one again.  A walk may have no
+    // places, and begin behind the view: splits are cut for the most tiles that any rows can see (view_tiles), and these may see fewer.
+    __host__ __device__ __forceinline__ int requested(int i, int tile0, int tile1) const { return tile(min(max(min(i, tile1 - 1), tile0), n_tiles - 1)); }
 };
 // whether some row at a position up to `last` does not see the start of tile `tile` for its window
-__device__ __forceinline__ bool before_window(const ChunkViewArgs& a, int tile, int last)
+__host__ __device__ __forceinline__ bool before_window(const ChunkViewArgs& a, int tile, int last)
 {
     return tile * kTileTokens <= last - a.window && tile * kTileTokens + kTileTokens > a.n_sink;
 }
-__device__ __forceinline__ bool in_window(const ChunkViewArgs& a, int tok, int pos) { return tok <= pos && (tok > pos - a.window || tok < a.n_sink); }
+__host__ __device__ __forceinline__ bool in_window(const ChunkViewArgs& a, int tok, int pos) { return tok <= pos && (tok > pos - a.window || tok < a.n_sink); }
 
 template <int ABID>
 __device__ __forceinline__ float4_t mfma_heads(half4_t q, half4_t k, float4_t c)
