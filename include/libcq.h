@@ -642,6 +642,8 @@ CQ_API cq_status cq_chunk_weights_paged(const void *q, const void *k_pool, const
  *   kept_lens         out, device int32 [batch]: min(t_n, keep), the sequence's length from then on (all its KV heads
  *                     keep as many tokens, each its own)
  *   workspace         device, cq_select_workspace_bytes(...) bytes; may be NULL for t <= 8192
+ *   kept, kept_lens and the workspace lie apart from each other, from weights and from seq_lens: lengths are not updated in
+ *   place (pass kept_lens as the seq_lens of the calls that follow)
  * The result is a function of the weights alone.
  *
  * cq_compact_cache   position r of stream (n, h) receives the codes (and, unless both are NULL, the accumulator) of

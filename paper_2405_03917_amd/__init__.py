@@ -1423,7 +1423,7 @@ def cq_select_tokens(weights, t: int, keep: int, n_sink: int = 0, n_recent: int 
                      workspace=None, stream=None):
     """The `keep` tokens that stay of every sequence and KV head: its first n_sink, its last n_recent, and the heaviest by
     `weights` fp32 [B, n_kv_heads, tokens].  Returns (kept int32 [B, n_kv_heads, keep], ascending, -1 behind the last; kept_lens
-    int32 [B], the sequences' new lengths)."""
+    int32 [B], the sequences' new lengths, in a tensor apart from seq_lens)."""
     return _on_stream(stream, prepare_select_tokens, weights, t, keep, n_sink, n_recent, seq_lens, kept, kept_lens, workspace)
 
 

@@ -1191,6 +1191,21 @@ size_t cq_select_workspace_bytes(int32_t batch, int32_t n_kv_heads, int32_t t)
     return runs * (sizeof(unsigned) * (kSelectCounts + kSelectRun) + sizeof(uint4)) + (size_t)batch * n_kv_heads * sizeof(uint2);
 }
 
+namespace {
+
+// an array of a call (no bytes: one that is not there)
+struct Span {
+    const void* at;
+    size_t bytes;
+};
+bool overlap(const Span& a, const Span& b)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    return a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
+
+}  // namespace
+
 cq_status cq_select_tokens(const float* weights, int64_t weights_stride, int32_t batch, int32_t n_kv_heads, int32_t t,
                            const int32_t* seq_lens, int32_t keep, int32_t n_sink, int32_t n_recent,
                            int32_t* kept, int32_t* kept_lens, void* workspace, size_t workspace_bytes, void* stream)
@@ -1204,6 +1219,18 @@ cq_status cq_select_tokens(const float* weights, int64_t weights_stride, int32_t
     if (parts > 1) {
         if (!workspace || !aligned16(workspace)) return CQ_ERR_INVALID_ARG;
         if (workspace_bytes < cq_select_workspace_bytes(batch, n_kv_heads, t)) return CQ_ERR_WORKSPACE_TOO_SMALL;
+    }
+    // What is written lies apart from what is read (a sequence's length is read by every KV head's workgroups, of every launch, and
+    // its new one written by one of the first) and from each other.
+    const size_t streams = (size_t)batch * n_kv_heads;
+    const Span written[] = {{kept, sizeof(int32_t) * streams * keep}, {kept_lens, sizeof(int32_t) * (size_t)batch},
+                            {workspace, parts > 1 ? cq_select_workspace_bytes(batch, n_kv_heads, t) : 0}};
+    const Span read[] = {{weights, sizeof(float) * ((streams - 1) * (size_t)weights_stride + t)}, {seq_lens, seq_lens ? sizeof(int32_t) * (size_t)batch : 0}};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (overlap(written[i], written[j])) return CQ_ERR_INVALID_ARG;
+        for (const Span& r : read)
+            if (overlap(written[i], r)) return CQ_ERR_INVALID_ARG;
     }
     SelectArgs a{weights, weights_stride, seq_lens, batch, n_kv_heads, t, keep, n_sink, n_recent, kept, kept_lens, parts};
     if (parts > 1) {
@@ -1221,12 +1248,6 @@ namespace {
 size_t compact_codes_bytes(const Derived& f, int32_t batch, int32_t keep)
 {
     return (size_t)2 * batch * f.n_kv_heads * ((keep + (size_t)kTileTokens - 1) / kTileTokens) * f.tile_bytes;
-}
-
-bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
-{
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + b_bytes && y < x + a_bytes;
 }
 
 cq_status compact_common(const void* k_codes, const void* v_codes, const float* weights, int64_t weights_stride, const cq_format* fmt,
@@ -1263,11 +1284,11 @@ cq_status compact_common(const void* k_codes, const void* v_codes, const float* 
     const size_t streams = (size_t)batch * f.n_kv_heads;
     const size_t w_bytes = weights ? sizeof(float) * ((streams - 1) * weights_stride + t) : 0;
     const size_t wo_bytes = weights ? sizeof(float) * ((streams - 1) * weights_out_stride + std::max(end, keep)) : 0;
-    if (overlap(k_codes, in_bytes, v_codes, in_bytes) || overlap(k_out, out_bytes, v_out, out_bytes)) return CQ_ERR_INVALID_ARG;
-    if (overlap(k_out, out_bytes, v_codes, in_bytes) || overlap(v_out, out_bytes, k_codes, in_bytes)) return CQ_ERR_INVALID_ARG;
-    if ((!same_k && overlap(k_out, out_bytes, k_codes, in_bytes)) || (!same_v && overlap(v_out, out_bytes, v_codes, in_bytes))) return CQ_ERR_INVALID_ARG;
+    if (overlap({k_codes, in_bytes}, {v_codes, in_bytes}) || overlap({k_out, out_bytes}, {v_out, out_bytes})) return CQ_ERR_INVALID_ARG;
+    if (overlap({k_out, out_bytes}, {v_codes, in_bytes}) || overlap({v_out, out_bytes}, {k_codes, in_bytes})) return CQ_ERR_INVALID_ARG;
+    if ((!same_k && overlap({k_out, out_bytes}, {k_codes, in_bytes})) || (!same_v && overlap({v_out, out_bytes}, {v_codes, in_bytes}))) return CQ_ERR_INVALID_ARG;
     if (!pages && (same_k || same_v) && t_cap_out != t_cap) return CQ_ERR_INVALID_ARG;
-    if (weights && (same_w ? weights_out_stride != weights_stride : overlap(weights_out, wo_bytes, weights, w_bytes))) return CQ_ERR_INVALID_ARG;
+    if (weights && (same_w ? weights_out_stride != weights_stride : overlap({weights_out, wo_bytes}, {weights, w_bytes}))) return CQ_ERR_INVALID_ARG;
     const bool in_place = same_k || same_v || same_w;
     // In place, place by place: a workgroup per stream moves its tokens forward, in one launch; long lists of few streams go through
     // the workspace, where all CUs take part.  Streams x tokens that stay, one workgroup a stream -> workspace, us: CQ-8c8b 8 x 4096
