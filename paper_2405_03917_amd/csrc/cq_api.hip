@@ -1282,13 +1282,20 @@ cq_status compact_common(const void* k_codes, const void* v_codes, const float* 
     // Each output is either its own input, moved in place, or apart from everything else.
     const bool same_k = k_out == k_codes, same_v = v_out == v_codes, same_w = weights && weights_out == weights;
     const size_t streams = (size_t)batch * f.n_kv_heads;
-    const size_t w_bytes = weights ? sizeof(float) * ((streams - 1) * weights_stride + t) : 0;
-    const size_t wo_bytes = weights ? sizeof(float) * ((streams - 1) * weights_out_stride + std::max(end, keep)) : 0;
-    if (overlap({k_codes, in_bytes}, {v_codes, in_bytes}) || overlap({k_out, out_bytes}, {v_out, out_bytes})) return CQ_ERR_INVALID_ARG;
-    if (overlap({k_out, out_bytes}, {v_codes, in_bytes}) || overlap({v_out, out_bytes}, {k_codes, in_bytes})) return CQ_ERR_INVALID_ARG;
-    if ((!same_k && overlap({k_out, out_bytes}, {k_codes, in_bytes})) || (!same_v && overlap({v_out, out_bytes}, {v_codes, in_bytes}))) return CQ_ERR_INVALID_ARG;
+    const Span in[] = {{k_codes, in_bytes}, {v_codes, in_bytes}, {weights, weights ? sizeof(float) * ((streams - 1) * weights_stride + t) : 0},
+                       {kept, sizeof(int32_t) * streams * keep}, {kept_lens, sizeof(int32_t) * (size_t)batch}};
+    const Span out[] = {{k_out, out_bytes}, {v_out, out_bytes},
+                        {weights_out, weights ? sizeof(float) * ((streams - 1) * weights_out_stride + std::max(end, keep)) : 0}};
+    const bool same[] = {same_k, same_v, same_w};
+    if (overlap(in[0], in[1])) return CQ_ERR_INVALID_ARG;
+    for (int o = 0; o < 3; ++o) {
+        for (int i = 0; i < 5; ++i)
+            if (!(i == o && same[o]) && overlap(out[o], in[i])) return CQ_ERR_INVALID_ARG;
+        for (int i = 0; i < o; ++i)
+            if (overlap(out[o], out[i])) return CQ_ERR_INVALID_ARG;
+    }
     if (!pages && (same_k || same_v) && t_cap_out != t_cap) return CQ_ERR_INVALID_ARG;
-    if (weights && (same_w ? weights_out_stride != weights_stride : overlap({weights_out, wo_bytes}, {weights, w_bytes}))) return CQ_ERR_INVALID_ARG;
+    if (same_w && weights_out_stride != weights_stride) return CQ_ERR_INVALID_ARG;
     const bool in_place = same_k || same_v || same_w;
     // In place, place by place: a workgroup per stream moves its tokens forward, in one launch; long lists of few streams go through
     // the workspace, where all CUs take part.  Streams x tokens that stay, one workgroup a stream -> workspace, us: CQ-8c8b 8 x 4096
@@ -1302,7 +1309,12 @@ cq_status compact_common(const void* k_codes, const void* v_codes, const float* 
     a.work_weights = nullptr;
     if (in_place) {                     // (asked for in either case: what a call needs does not follow a choice of kernels)
         if (!workspace) return CQ_ERR_INVALID_ARG;
-        if (workspace_bytes < codes + sizeof(float) * streams * keep) return CQ_ERR_WORKSPACE_TOO_SMALL;
+        const Span work{workspace, codes + sizeof(float) * streams * keep};
+        if (workspace_bytes < work.bytes) return CQ_ERR_WORKSPACE_TOO_SMALL;
+        for (const Span& x : in)
+            if (overlap(work, x)) return CQ_ERR_INVALID_ARG;
+        for (const Span& x : out)
+            if (overlap(work, x)) return CQ_ERR_INVALID_ARG;
         a.work = a.slide ? nullptr : static_cast<uint8_t*>(workspace);
         a.work_weights = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + codes);
     }
