@@ -1457,8 +1457,9 @@ def prepare_compact_cache(k_codes, v_codes, weights, fmt: CQFormat, kept, kept_l
         stride_out = _check_weights(weights_out, batch, fmt, max(keep, min(t, t_cap_out if pages_out is None else 64 * pages_out.max_tiles)), "weights_out")
     elif weights_out is not None:
         raise ValueError("weights_out goes with weights")
-    if k_out is k_codes or v_out is v_codes or (weights is not None and weights_out is weights) or workspace is not None \
-            or k_out.data_ptr() == k_codes.data_ptr() or v_out.data_ptr() == v_codes.data_ptr():
+    # (by address, as the library compares them: an output may be its input under another tensor object)
+    in_place = any(x is not None and x.data_ptr() == y.data_ptr() for x, y in ((k_codes, k_out), (v_codes, v_out), (weights, weights_out)))
+    if in_place or workspace is not None:
         workspace = _workspace(workspace, cq_compact_workspace_bytes(fmt, batch, keep), kept.device, "cq_compact_workspace_bytes")
     _same_device(k_codes, v_codes, weights, kept, kept_lens, k_out, v_out, weights_out, workspace,
                  None if pages is None else pages.block_table, None if pages_out is None else pages_out.block_table)
