@@ -9,6 +9,7 @@ works but the first call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -281,6 +282,50 @@ def _stream_handle(stream) -> int:
     return int(stream.cuda_stream)
 
 
+def _tensors(x):
+    """The tensors that an argument or a result of a call holds."""
+    import torch
+    if isinstance(x, torch.Tensor):
+        yield x
+    elif isinstance(x, PageTable):
+        yield x.block_table
+    elif isinstance(x, RopeTable):
+        yield x.table
+    elif isinstance(x, LayerTable):
+        yield x.table
+        yield from _tensors(x._keep)
+    elif isinstance(x, dict):
+        yield from _tensors(tuple(x.values()))
+    elif isinstance(x, (tuple, list)):
+        for y in x:
+            yield from _tensors(y)
+
+
+def _on_stream(fn):
+    """A call that takes `stream` (a torch stream; None: the current one).  What is allocated for it comes from that stream's
+    memory pool: work on the current stream that still uses memory freed there is not in its way, nor is what is allocated
+    there next.  Its arguments are recorded on the stream: one that the caller drops is not handed out again before
+    the call is done with it; what it returns is recorded on the caller's stream.  (The caller orders the streams: what
+    the call reads has to be written before `stream` comes to it.)"""
+    at = fn.__code__.co_varnames[:fn.__code__.co_argcount].index("stream")
+
+    @functools.wraps(fn)
+    def call(*args, **kwargs):
+        stream = kwargs["stream"] if "stream" in kwargs else args[at] if len(args) > at else None
+        if stream is None:
+            return fn(*args, **kwargs)
+        import torch
+        user = torch.cuda.current_stream()
+        with torch.cuda.stream(stream):
+            result = fn(*args, **kwargs)
+        for x in _tensors((args, kwargs)):
+            x.record_stream(stream)
+        for x in _tensors((result, args[0]) if fn.__name__ == "__init__" else result):
+            x.record_stream(user)
+        return result
+    return call
+
+
 def _dev(t, dtype, what: str):
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -301,7 +346,8 @@ def alloc_cache(fmt: CQFormat, batch: int, t_cap: int, device="cuda"):
 
 class PreparedCall:
     """An entry point with its arguments marshalled once: ``call()`` (or ``call(stream)``) only
-    crosses the C ABI.  Keeps the tensors it points into alive."""
+    crosses the C ABI.  Keeps the tensors it points into alive: a call on a stream that is not theirs is kept
+    until that stream is done with it."""
     __slots__ = ("_fn", "_args", "_keep", "_name")
 
     def __init__(self, fn, args, keep, name):
@@ -361,12 +407,14 @@ def prepare_encode_kv(x_k, x_v, k_centroids, v_centroids, fmt: CQFormat, k_codes
     return PreparedCall(load().cq_encode_kv, args, keep, "cq_encode_kv")
 
 
+@_on_stream
 def cq_encode_kv(x_k, x_v, k_centroids, v_centroids, fmt: CQFormat, k_codes, v_codes, t_offset: int, t_cap: int,
                  stream=None) -> None:
     """cq_encode of a key and a value tensor of the same shape in one launch."""
     prepare_encode_kv(x_k, x_v, k_centroids, v_centroids, fmt, k_codes, v_codes, t_offset, t_cap)(stream)
 
 
+@_on_stream
 def cq_encode(x, centroids, fmt: CQFormat, codes, t_offset: int, t_cap: int, stream=None) -> None:
     """x fp16 [B, T_new, D] (last dim contiguous), centroids fp16 [G, 2^b, c] contiguous,
     codes uint8 packed cache; writes the codes of the new tokens at positions t_offset..."""
@@ -458,6 +506,7 @@ def prepare_decode_attention_static(q, k_codes, v_codes, k_centroids, v_centroid
     return PreparedCall(load().cq_decode_attention_static, args, keep, "cq_decode_attention_static")
 
 
+@_on_stream
 def cq_decode_attention_static(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat,
                                t: int, t_cap: int, out, seq_lens=None, tokens_per_split: int = 0, stream=None):
     """cq_decode_attention without a workspace (the library's static scratch array holds the
@@ -467,6 +516,7 @@ def cq_decode_attention_static(q, k_codes, v_codes, k_centroids, v_centroids, sc
     return out
 
 
+@_on_stream
 def cq_decode_attention(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat,
                         t: int, t_cap: int, seq_lens=None, tokens_per_split: int = 0,
                         out=None, workspace=None, stream=None):
@@ -488,6 +538,7 @@ def cq_fused_format(fmt: CQFormat) -> CQFormat:
     return CQFormat(out.c, out.b, out.head_dim, out.n_kv_heads)
 
 
+@_on_stream
 def cq_expand_codebook(centroids, fmt: CQFormat, out=None, stream=None):
     """Sub-byte codebook fp16 [G, 2^b, c] -> the fused format's codebook fp16 [G b/8, 256, 8 c/b]."""
     import torch
@@ -561,6 +612,7 @@ def prepare_chunk_attention(q, k_codes, v_codes, k_centroids, v_centroids, scale
     return PreparedCall(load().cq_chunk_attention, head + (t_cap,) + tail, keep, "cq_chunk_attention"), out
 
 
+@_on_stream
 def cq_chunk_attention(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int,
                        seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None, stream=None):
     """Causal attention of the last m tokens of each sequence over its cache: q, out fp16
@@ -571,6 +623,7 @@ def cq_chunk_attention(q, k_codes, v_codes, k_centroids, v_centroids, scale: flo
     return out
 
 
+@_on_stream
 def cq_chunk_attention_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int, pages,
                              seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None, stream=None):
     """cq_chunk_attention over paged pools."""
@@ -586,6 +639,7 @@ class LayerTable:
     out [B, Hq, head_dim] (as for cq_decode_step; all layers share shapes and the row stride)."""
     FIELDS = ("q", "x_k_new", "x_v_new", "k_codes", "v_codes", "k_centroids", "v_centroids", "out")
 
+    @_on_stream
     def __init__(self, layers, fmt: CQFormat, t_cap: int, stream=None):
         import torch
         if not layers:
@@ -654,6 +708,7 @@ def prepare_decode_step_layers(table: LayerTable, scale: float, t: int, seq_lens
     return PreparedCall(load().cq_decode_step_layers, args, (table, seq_lens, workspace, f), "cq_decode_step_layers")
 
 
+@_on_stream
 def cq_decode_step_layers(table: LayerTable, scale: float, t: int, seq_lens=None, tokens_per_split: int = 0,
                           workspace=None, stream=None):
     """cq_decode_step of every layer of the table in one launch; returns the layers' out tensors."""
@@ -664,6 +719,7 @@ def cq_decode_step_layers(table: LayerTable, scale: float, t: int, seq_lens=None
 class RopeTable:
     """The trigonometric table of cq_rope_table on the device: covers positions [0, positions)."""
 
+    @_on_stream
     def __init__(self, base: float, positions: int, head_dim: int = 128, device="cuda", stream=None):
         import torch
         nbytes = int(load().cq_rope_table_bytes(head_dim, positions))
@@ -710,6 +766,7 @@ def prepare_chunk_attention_rope(q, k_codes, v_codes, k_centroids, v_centroids, 
     return PreparedCall(getattr(load(), name), args, call._keep + (rope,), name), out
 
 
+@_on_stream
 def cq_chunk_attention_rope(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int,
                             rope: "RopeTable", seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None, stream=None):
     """cq_chunk_attention for caches whose keys were quantized before RoPE (token by token through
@@ -720,6 +777,7 @@ def cq_chunk_attention_rope(q, k_codes, v_codes, k_centroids, v_centroids, scale
     return out
 
 
+@_on_stream
 def cq_chunk_attention_rope_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int, pages,
                                   rope: "RopeTable", seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None,
                                   stream=None):
@@ -746,6 +804,7 @@ def prepare_decode_attention_rope(q, k_codes, v_codes, k_centroids, v_centroids,
     return PreparedCall(load().cq_decode_attention_rope, args, call._keep + (rope,), "cq_decode_attention_rope"), out
 
 
+@_on_stream
 def cq_decode_attention_rope(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat,
                              t: int, t_cap: int, rope: RopeTable, seq_lens=None, tokens_per_split: int = 0,
                              out=None, workspace=None, stream=None):
@@ -773,6 +832,7 @@ def prepare_decode_step_rope(q, x_k_new, x_v_new, k_codes, v_codes, k_centroids,
     return PreparedCall(load().cq_decode_step_rope, args, call._keep + (rope,), "cq_decode_step_rope"), out
 
 
+@_on_stream
 def cq_decode_step_rope(q, x_k_new, x_v_new, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat,
                         t: int, t_cap: int, rope: RopeTable, seq_lens=None, tokens_per_split: int = 0, out=None,
                         workspace=None, stream=None):
@@ -804,6 +864,7 @@ def prepare_decode_step(q, x_k_new, x_v_new, k_codes, v_codes, k_centroids, v_ce
     return PreparedCall(load().cq_decode_step, args, keep, "cq_decode_step"), out
 
 
+@_on_stream
 def cq_decode_step(q, x_k_new, x_v_new, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat,
                    t: int, t_cap: int, seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None,
                    stream=None):
@@ -815,6 +876,7 @@ def cq_decode_step(q, x_k_new, x_v_new, k_codes, v_codes, k_centroids, v_centroi
     return out
 
 
+@_on_stream
 def cq_probe_stream_read(src, sink, stream=None) -> None:
     """Read every byte of the uint8 device tensor `src` once (measurement aid)."""
     import torch
@@ -827,6 +889,7 @@ def cq_probe_stream_read(src, sink, stream=None) -> None:
         raise CQError(st, "cq_probe_stream_read")
 
 
+@_on_stream
 def cq_probe_copy(src, dst, stream=None) -> None:
     """dst[:] = src for uint8 device tensors of equal size (measurement aid)."""
     import torch
@@ -884,6 +947,7 @@ def _check_centroids(fmt: CQFormat, k_centroids, v_centroids) -> None:
             raise ValueError(f"{name} must be contiguous [G, 2^b, c]")
 
 
+@_on_stream
 def cq_encode_kv_paged(x_k, x_v, k_centroids, v_centroids, fmt: CQFormat, k_pool, v_pool, pages: PageTable,
                        t_offset: int, stream=None) -> None:
     """cq_encode_kv into paged pools: x fp16 [B, T_new, D]; tokens go to positions t_offset ... of
@@ -963,6 +1027,7 @@ def _paged_decode(fn_name, q, x_k_new, x_v_new, k_pool, v_pool, k_centroids, v_c
     return out
 
 
+@_on_stream
 def cq_decode_attention_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
                               pages: PageTable, seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None,
                               stream=None):
@@ -971,6 +1036,7 @@ def cq_decode_attention_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale
                          t, pages, seq_lens, tokens_per_split, out, workspace, stream)
 
 
+@_on_stream
 def cq_decode_attention_rope_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
                                    pages: PageTable, rope: RopeTable, seq_lens=None, tokens_per_split: int = 0,
                                    out=None, workspace=None, stream=None):
@@ -979,6 +1045,7 @@ def cq_decode_attention_rope_paged(q, k_pool, v_pool, k_centroids, v_centroids, 
                          scale, fmt, t, pages, seq_lens, tokens_per_split, out, workspace, stream, rope=rope)
 
 
+@_on_stream
 def cq_decode_step_rope_paged(q, x_k_new, x_v_new, k_pool, v_pool, k_centroids, v_centroids, scale: float,
                               fmt: CQFormat, t: int, pages: PageTable, rope: RopeTable, seq_lens=None,
                               tokens_per_split: int = 0, out=None, workspace=None, stream=None):
@@ -987,6 +1054,7 @@ def cq_decode_step_rope_paged(q, x_k_new, x_v_new, k_pool, v_pool, k_centroids, 
                          scale, fmt, t, pages, seq_lens, tokens_per_split, out, workspace, stream, rope=rope)
 
 
+@_on_stream
 def cq_decode_step_paged(q, x_k_new, x_v_new, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat,
                          t: int, pages: PageTable, seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None,
                          stream=None):
@@ -995,6 +1063,7 @@ def cq_decode_step_paged(q, x_k_new, x_v_new, k_pool, v_pool, k_centroids, v_cen
                          fmt, t, pages, seq_lens, tokens_per_split, out, workspace, stream)
 
 
+@_on_stream
 def cq_dequantize(codes, centroids, fmt: CQFormat, batch: int, t_offset: int, t_count: int, t_cap: int, out=None,
                   stream=None):
     """fp16 [batch, t_count, D] = the centroids the cached codes of positions t_offset .. t_offset +
@@ -1025,6 +1094,7 @@ def cq_kmeans_workspace_bytes(fmt: CQFormat, n_points: int) -> int:
     return n
 
 
+@_on_stream
 def cq_kmeans_fit(x, fmt: CQFormat, n_iter: int, rnd=None, init_centroids=None, weights=None,
                   want_picks: bool = False, want_assignment: bool = False, workspace=None, stream=None) -> dict:
     """Centroid learning for every channel group of x fp16 [n, D] (device): k-means++ from the
@@ -1073,6 +1143,7 @@ def cq_kmeans_fit(x, fmt: CQFormat, n_iter: int, rnd=None, init_centroids=None, 
     return out
 
 
+@_on_stream
 def cq_probe_mfma(a, b, stream=None):
     """D = A B by one matrix-core instruction: a fp16 [32, kdim], b fp16 [kdim, 32] (kdim 8 or 16,
     contiguous device tensors) -> fp32 [32, 32] (measurement aid)."""
@@ -1091,21 +1162,11 @@ def cq_probe_mfma(a, b, stream=None):
 
 # ---------------------------------------------------------------- caches that stay bounded
 
-def _on_stream(stream, prepare, *args, **kwargs) -> tuple:
-    """Prepare a call and make it on `stream`, whose memory pool what is allocated for it comes from: work on the current stream
-    that still uses memory freed there is not in its way, nor is what is allocated there next.  Returns the outputs."""
-    import torch
-    if stream is None:
-        made = prepare(*args, **kwargs)
-    else:
-        user = torch.cuda.current_stream()
-        with torch.cuda.stream(stream):
-            made = prepare(*args, **kwargs)
+def _run(stream, prepare, *args, **kwargs) -> tuple:
+    """Prepare a call and make it; returns its outputs."""
+    made = prepare(*args, **kwargs)
     call, outs = (made, ()) if isinstance(made, PreparedCall) else (made[0], tuple(made[1:]))
     call(stream)
-    if stream is not None:
-        for out in outs:
-            out.record_stream(user)
     return outs
 
 
@@ -1226,40 +1287,44 @@ def prepare_decode_attention_window(q, k_codes, v_codes, k_centroids, v_centroid
     return PreparedCall(getattr(load(), name), head + args, keep, name), out
 
 
+@_on_stream
 def cq_decode_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int,
                                window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None,
                                stream=None):
     """cq_decode_attention through a sliding window: the last `window` tokens of each sequence and its first `n_sink`."""
-    return _on_stream(stream, prepare_decode_attention_window, q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t,
-                      t_cap, window, n_sink, None, seq_lens, tokens_per_split, out, workspace)[0]
+    return _run(stream, prepare_decode_attention_window, q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t,
+                t_cap, window, n_sink, None, seq_lens, tokens_per_split, out, workspace)[0]
 
 
+@_on_stream
 def cq_decode_attention_window_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
                                      pages: PageTable, window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0,
                                      out=None, workspace=None, stream=None):
     """cq_decode_attention_window over paged pools (pages outside the window and the sinks are not looked at)."""
-    return _on_stream(stream, prepare_decode_attention_window, q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0,
-                      window, n_sink, pages, seq_lens, tokens_per_split, out, workspace)[0]
+    return _run(stream, prepare_decode_attention_window, q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0,
+                window, n_sink, pages, seq_lens, tokens_per_split, out, workspace)[0]
 
 
+@_on_stream
 def cq_decode_step_window(q, x_k_new, x_v_new, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
                           t_cap: int, window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0, out=None,
                           workspace=None, stream=None):
     """cq_decode_step through a sliding window with sinks: the new token is encoded at position t - 1 (seq_lens[n] - 1)."""
     if x_k_new is None or x_v_new is None:
         raise TypeError("x_k_new and x_v_new must be CUDA/HIP tensors")
-    return _on_stream(stream, prepare_decode_attention_window, q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t,
-                      t_cap, window, n_sink, None, seq_lens, tokens_per_split, out, workspace, x_k_new, x_v_new)[0]
+    return _run(stream, prepare_decode_attention_window, q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t,
+                t_cap, window, n_sink, None, seq_lens, tokens_per_split, out, workspace, x_k_new, x_v_new)[0]
 
 
+@_on_stream
 def cq_decode_step_window_paged(q, x_k_new, x_v_new, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
                                 pages: PageTable, window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0, out=None,
                                 workspace=None, stream=None):
     """cq_decode_step_window over paged pools."""
     if x_k_new is None or x_v_new is None:
         raise TypeError("x_k_new and x_v_new must be CUDA/HIP tensors")
-    return _on_stream(stream, prepare_decode_attention_window, q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0,
-                      window, n_sink, pages, seq_lens, tokens_per_split, out, workspace, x_k_new, x_v_new)[0]
+    return _run(stream, prepare_decode_attention_window, q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0,
+                window, n_sink, pages, seq_lens, tokens_per_split, out, workspace, x_k_new, x_v_new)[0]
 
 
 def cq_chunk_window_workspace_bytes(fmt: CQFormat, batch: int, n_q_heads: int, m: int, t: int, window: int, n_sink: int = 0,
@@ -1292,21 +1357,23 @@ def prepare_chunk_attention_window(q, k_codes, v_codes, k_centroids, v_centroids
     return PreparedCall(getattr(load(), name), args, keep, name), out
 
 
+@_on_stream
 def cq_chunk_attention_window(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int,
                               window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None,
                               stream=None):
     """cq_chunk_attention through sliding windows: each of the last m tokens sees the `window` tokens up to its own position
     and the sequence's first `n_sink`."""
-    return _on_stream(stream, prepare_chunk_attention_window, q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t, t_cap,
-                      window, n_sink, None, seq_lens, tokens_per_split, out, workspace)[0]
+    return _run(stream, prepare_chunk_attention_window, q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t, t_cap,
+                window, n_sink, None, seq_lens, tokens_per_split, out, workspace)[0]
 
 
+@_on_stream
 def cq_chunk_attention_window_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
                                     pages: PageTable, window: int, n_sink: int = 0, seq_lens=None, tokens_per_split: int = 0,
                                     out=None, workspace=None, stream=None):
     """cq_chunk_attention_window over paged pools."""
-    return _on_stream(stream, prepare_chunk_attention_window, q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0,
-                      window, n_sink, pages, seq_lens, tokens_per_split, out, workspace)[0]
+    return _run(stream, prepare_chunk_attention_window, q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0,
+                window, n_sink, pages, seq_lens, tokens_per_split, out, workspace)[0]
 
 
 def cq_decode_weights_workspace_bytes(fmt: CQFormat, batch: int, n_q_heads: int, t: int, tokens_per_split: int = 0) -> int:
@@ -1331,21 +1398,23 @@ def prepare_decode_attention_weights(q, k_codes, v_codes, k_centroids, v_centroi
     return PreparedCall(getattr(load(), name), args, keep, name), out
 
 
+@_on_stream
 def cq_decode_attention_weights(q, k_codes, v_codes, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int,
                                 weights, decay: float = 1.0, seq_lens=None, tokens_per_split: int = 0, out=None, workspace=None,
                                 stream=None):
     """cq_decode_attention that also adds each cached token's attention weight, summed over the query heads of its KV head, to
     `weights` fp32 [B, n_kv_heads, tokens]: weights = decay weights + this step's (decay 0: weights are not read)."""
-    return _on_stream(stream, prepare_decode_attention_weights, q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t,
-                      t_cap, weights, decay, None, seq_lens, tokens_per_split, out, workspace)[0]
+    return _run(stream, prepare_decode_attention_weights, q, k_codes, v_codes, k_centroids, v_centroids, scale, fmt, t,
+                t_cap, weights, decay, None, seq_lens, tokens_per_split, out, workspace)[0]
 
 
+@_on_stream
 def cq_decode_attention_weights_paged(q, k_pool, v_pool, k_centroids, v_centroids, scale: float, fmt: CQFormat, t: int,
                                       pages: PageTable, weights, decay: float = 1.0, seq_lens=None, tokens_per_split: int = 0,
                                       out=None, workspace=None, stream=None):
     """cq_decode_attention_weights over paged pools."""
-    return _on_stream(stream, prepare_decode_attention_weights, q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0,
-                      weights, decay, pages, seq_lens, tokens_per_split, out, workspace)[0]
+    return _run(stream, prepare_decode_attention_weights, q, k_pool, v_pool, k_centroids, v_centroids, scale, fmt, t, 0,
+                weights, decay, pages, seq_lens, tokens_per_split, out, workspace)[0]
 
 
 def cq_chunk_weights_workspace_bytes(fmt: CQFormat, batch: int, n_q_heads: int, m: int, t: int) -> int:
@@ -1374,19 +1443,21 @@ def prepare_chunk_weights(q, k_codes, k_centroids, scale: float, fmt: CQFormat, 
     return PreparedCall(getattr(load(), name), args, (q, k_codes, k_centroids, seq_lens, weights, workspace, f, pages), name)
 
 
+@_on_stream
 def cq_chunk_weights(q, k_codes, k_centroids, scale: float, fmt: CQFormat, t: int, t_cap: int, weights, decay: float = 1.0,
                      seq_lens=None, workspace=None, stream=None) -> None:
     """weights fp32 [B, n_kv_heads, tokens] = decay weights + the causal attention weights of the last m tokens of each sequence,
     summed over them and over the query heads of each KV head; q fp16 [B, m, Hq, head_dim]."""
-    _on_stream(stream, prepare_chunk_weights, q, k_codes, k_centroids, scale, fmt, t, t_cap, weights, decay, None, seq_lens,
-               workspace)
+    _run(stream, prepare_chunk_weights, q, k_codes, k_centroids, scale, fmt, t, t_cap, weights, decay, None, seq_lens,
+         workspace)
 
 
+@_on_stream
 def cq_chunk_weights_paged(q, k_pool, k_centroids, scale: float, fmt: CQFormat, t: int, pages: PageTable, weights, decay: float = 1.0,
                            seq_lens=None, workspace=None, stream=None) -> None:
     """cq_chunk_weights over a paged key pool."""
-    _on_stream(stream, prepare_chunk_weights, q, k_pool, k_centroids, scale, fmt, t, 0, weights, decay, pages, seq_lens,
-               workspace)
+    _run(stream, prepare_chunk_weights, q, k_pool, k_centroids, scale, fmt, t, 0, weights, decay, pages, seq_lens,
+         workspace)
 
 
 def cq_select_workspace_bytes(batch: int, n_kv_heads: int, t: int) -> int:
@@ -1419,12 +1490,13 @@ def prepare_select_tokens(weights, t: int, keep: int, n_sink: int = 0, n_recent:
     return PreparedCall(load().cq_select_tokens, args, (weights, seq_lens, kept, kept_lens, workspace), "cq_select_tokens"), kept, kept_lens
 
 
+@_on_stream
 def cq_select_tokens(weights, t: int, keep: int, n_sink: int = 0, n_recent: int = 0, seq_lens=None, kept=None, kept_lens=None,
                      workspace=None, stream=None):
     """The `keep` tokens that stay of every sequence and KV head: its first n_sink, its last n_recent, and the heaviest by
     `weights` fp32 [B, n_kv_heads, tokens].  Returns (kept int32 [B, n_kv_heads, keep], ascending, -1 behind the last; kept_lens
     int32 [B], the sequences' new lengths, in a tensor apart from seq_lens)."""
-    return _on_stream(stream, prepare_select_tokens, weights, t, keep, n_sink, n_recent, seq_lens, kept, kept_lens, workspace)
+    return _run(stream, prepare_select_tokens, weights, t, keep, n_sink, n_recent, seq_lens, kept, kept_lens, workspace)
 
 
 def cq_compact_workspace_bytes(fmt: CQFormat, batch: int, keep: int) -> int:
@@ -1474,16 +1546,18 @@ def prepare_compact_cache(k_codes, v_codes, weights, fmt: CQFormat, kept, kept_l
     return PreparedCall(getattr(load(), name), args, keep_alive, name)
 
 
+@_on_stream
 def cq_compact_cache(k_codes, v_codes, weights, fmt: CQFormat, kept, kept_lens, t: int, t_cap: int, k_out=None, v_out=None,
                      weights_out=None, t_cap_out=None, workspace=None, stream=None) -> None:
     """Move the tokens `kept` (cq_select_tokens) of every sequence and KV head, codes and accumulators (weights None: codes
     alone), to positions 0, 1, ...: in place, or into k_out, v_out, weights_out of capacity t_cap_out."""
-    _on_stream(stream, prepare_compact_cache, k_codes, v_codes, weights, fmt, kept, kept_lens, t, t_cap, k_out, v_out,
-               weights_out, t_cap_out, workspace=workspace)
+    _run(stream, prepare_compact_cache, k_codes, v_codes, weights, fmt, kept, kept_lens, t, t_cap, k_out, v_out,
+         weights_out, t_cap_out, workspace=workspace)
 
 
+@_on_stream
 def cq_compact_cache_paged(k_pool, v_pool, weights, fmt: CQFormat, kept, kept_lens, t: int, pages: PageTable, k_pool_out=None,
                            v_pool_out=None, weights_out=None, pages_out=None, workspace=None, stream=None) -> None:
     """cq_compact_cache from the pages of `pages` to those of `pages_out` (default: in place)."""
-    _on_stream(stream, prepare_compact_cache, k_pool, v_pool, weights, fmt, kept, kept_lens, t, 0, k_pool_out, v_pool_out,
-               weights_out, 0, pages, pages_out, workspace)
+    _run(stream, prepare_compact_cache, k_pool, v_pool, weights, fmt, kept, kept_lens, t, 0, k_pool_out, v_pool_out,
+         weights_out, 0, pages, pages_out, workspace)
