@@ -401,13 +401,18 @@ cq_status launch_decode_view(const DecodeViewArgs& a_in, hipStream_t stream)
     DecodeViewArgs a = a_in;
     if (decode_takes_quads(a_in, view_tiles(a_in.t, 1, a_in.window, a_in.n_sink), &a)) return launch_decode_quad_view(a, stream);
     // With the scores kept, the weights need all splits of a row and all query heads of a KV head.  One query head and a short
-    // context, or one of medium length where other rows' workgroups run meanwhile: the row's last workgroup adds them up as it merges
-    // the output.  Otherwise a kernel of its own, which merges too.  32 heads, a kernel of its own -> here, us (in launches back to back):
-    // CQ-8c8b 1 x 100 9.8 -> 7.3, 1 x 2000 9.9 -> 9.8, 1 x 4096 10.4 -> 10.7, 1 x 16384 12.9 -> 12.9 (there the kernel), 8 x 2000 12.6 ->
-    // 10.6, 8 x 8192 25.5 -> 22.7, 8 x 16384 42.5 -> 40.7, 32 x 4096 44.6 -> 43.4; CQ-4c8b 8 x 4096 21.6 -> 19.6; CQ-2c8b 1 x 1000 14.4 -> 13.1,
-    // 8 x 8192 58.8 -> 59.2; CQ-8c10b 1 x 1000 13.1 -> 11.8, 8 x 8192 39.4 -> 41.2.
+    // context: the row's last workgroup adds them up as it merges the output; so, too, over contexts of medium length where 256 rows
+    // run meanwhile, of the formats whose walk goes by chunks (the others gain and lose 5 % there).  Otherwise a kernel of its own, which
+    // merges too.  32 heads, a kernel of its own -> here, us (in launches back to back):
+    //   CQ-8c8b   1 x 100 10.6 -> 7.6, 1 x 2000 10.5 -> 10.3, 1 x 3000 11.2 -> 11.2, 1 x 4096 10.9 -> 11.1, 4 x 4096 14.1 -> 14.0, 8 x 2000 13.9 ->
+    //             11.8, 8 x 4096 16.3 -> 15.0, 8 x 16384 43.1 -> 41.4, 32 x 4096 45.5 -> 43.6
+    //   CQ-4c8b   1 x 100 10.1 -> 8.0, 1 x 2000 12.1 -> 11.8, 1 x 4096 12.1 -> 12.4, 4 x 4096 16.4 -> 16.5, 8 x 4096 22.2 -> 21.1, 8 x 16384 68.0 -> 63.9
+    //   CQ-2c8b   1 x 1000 15.1 -> 13.5, 1 x 2000 15.3 -> 15.3, 1 x 4096 15.6 -> 16.1, 8 x 2000 22.8 -> 21.6, 8 x 4096 34.7 -> 34.4, 8 x 16384 109.3 -> 110.6
+    //   CQ-8c10b  1 x 1000 16.8 -> 15.3, 1 x 2000 16.2 -> 16.3, 1 x 4096 15.9 -> 16.9, 8 x 2000 24.2 -> 24.7, 16 x 2000 30.1 -> 28.8, 8 x 8192 40.4 -> 42.0,
+    //             16 x 8192 58.3 -> 55.6
     const int rows = a.batch * a.n_q_heads;
-    const bool short_rows = a.scores && a.n_q_heads == a.f.n_kv_heads && (a.t <= 4096 || (a.t <= 16384 && rows >= 256));
+    const bool by_chunks = a.f.b == 8 && a.f.gh <= 32;
+    const bool short_rows = a.scores && a.n_q_heads == a.f.n_kv_heads && (a.t <= 2048 || (a.t <= 16384 && rows >= 256 && by_chunks));
     a.merge_counters = a.n_split > 1 && (!a.scores || short_rows) ? g_merge_counters.for_stream(stream, a.batch * a.n_q_heads) : nullptr;
     a.finish = short_rows && (a.n_split == 1 || a.merge_counters);
     const cq_status st = decode_takes_pairs(a) ? launch_decode_pair_view(a, stream)
