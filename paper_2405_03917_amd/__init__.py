@@ -306,15 +306,17 @@ def _on_stream(fn):
     memory pool: work on the current stream that still uses memory freed there is not in its way, nor is what is allocated
     there next.  Its arguments are recorded on the stream: one that the caller drops is not handed out again before
     the call is done with it; what it returns is recorded on the caller's stream.  (The caller orders the streams: what
-    the call reads has to be written before `stream` comes to it.)"""
+    the call reads has to be written before `stream` comes to it.)  Another library's stream, an object with a
+    `cuda_stream`, may be gone when a tensor is freed: nothing is recorded on it, and the caller keeps what the call uses, a
+    workspace and outputs of its own among it, until it is done."""
     at = fn.__code__.co_varnames[:fn.__code__.co_argcount].index("stream")
 
     @functools.wraps(fn)
     def call(*args, **kwargs):
-        stream = kwargs["stream"] if "stream" in kwargs else args[at] if len(args) > at else None
-        if stream is None:
-            return fn(*args, **kwargs)
         import torch
+        stream = kwargs["stream"] if "stream" in kwargs else args[at] if len(args) > at else None
+        if not isinstance(stream, torch.cuda.Stream):
+            return fn(*args, **kwargs)
         user = torch.cuda.current_stream()
         with torch.cuda.stream(stream):
             result = fn(*args, **kwargs)

@@ -38,7 +38,7 @@ class _Lib:
     """The library with its launches left out."""
 
     def __init__(self, real):
-        self.real, self.launched = real, []
+        self.real, self.launched, self.on = real, [], []
 
     def __getattr__(self, name):
         if name.endswith(("_bytes", "_split", "_check", "_format", "_string")):
@@ -46,12 +46,14 @@ class _Lib:
 
         def launch(*args):
             self.launched.append(name)
+            self.on.append(args[-1])
             return cq.CQ_OK
         return launch
 
 
 class _Stream:
-    cuda_stream = 7
+    def __init__(self, cuda_stream=7):
+        self.cuda_stream = cuda_stream
 
 
 @pytest.fixture
@@ -71,6 +73,7 @@ def streams(on_host, monkeypatch):
 
     empty, allocated = torch.empty, []
     monkeypatch.setattr(cq, "load", lambda: lib)
+    monkeypatch.setattr(torch.cuda, "Stream", _Stream)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: current[-1])
     monkeypatch.setattr(torch.cuda, "stream", Switch)
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, stream: records.add((self.data_ptr(), stream)))
@@ -137,3 +140,14 @@ def test_a_call_on_another_stream_keeps_what_it_uses(streams, name):
     records.clear()
     call(operands, None)                                    # on the current stream: nothing to record
     assert not records
+
+
+def test_a_stream_of_another_library(streams):
+    class Theirs:
+        cuda_stream = 11
+
+    _, _, records, lib, _ = streams
+    operands = _operands()
+    cq.cq_decode_attention(operands["q"], operands["k"], operands["v"], operands["ck"], operands["cv"], 0.1, FMT, 300, 512, stream=Theirs())
+    assert lib.launched and lib.on == [11]
+    assert not records                                      # it may be gone when they are freed
