@@ -9,9 +9,10 @@
 // cq_compact_cache.  The token of rank r moves to position r.  A record's bytes are rotated by its token's position in
 // the tile (slot s of token u holds group (s + u) mod Gh), so a move from u to u' rotates the record by u' - u bytes
 // (10-bit codes: the word of high bits by twice as many bits).  A lane moves a token's record.
-// Bound by the chain of requests and barriers of each launch rather than by its bytes.  32 streams of 131072 tokens to 2047: counts 7.3
-// us, lists 9.4, positions 12.4, the move 5.4 (17 MB of weights, 4 MB moved); 512 streams of 4160 to 4096: selection 15, the move in
-// place 18.
+// Bound by the chain of requests and barriers of each launch where little moves, else by the bytes moved.  32 streams of 131072 tokens to
+// 2047: counts 7.3 us, lists 9.4, positions 12.4, the move 5.4 (17 MB of weights, 4 MB moved).  512 streams of 4160 to 4096 in place:
+// selection 12 to 14; the move of CQ-4c8b 10 to 12 where a sixth of the tokens change their place, 60 where nearly all do (281 MB read and
+// written, 4.7 TB/s; a copy reaches 5.18), of CQ-8c8b then 34, of CQ-2c8b 112.
 #include "cq_decode_common.hpp"
 
 namespace cq {
