@@ -678,6 +678,106 @@ CQ_API cq_status cq_compact_cache_paged(const void *k_pool, const void *v_pool, 
                                  void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * The 8-bit block cache: keys and values in 8 bits, with one scale for each block of 64 tokens and head, for layers (or
+ * models) that keep more precision than the codes above.  What fills it (rotating keys and queries to their positions on the
+ * way), what attends to it, and dense rows of it; contiguous, or paged like the caches above.
+ *
+ * A tile is the 64 tokens of one KV head: 8192 bytes of keys, [token][channel], and 8192 of values, [channel][token] (the
+ * order in which each enters its matrix product).  Tiles lie [sequence][KV head][tile] with t_cap / 64 tiles per stream, or,
+ * paged, [page][KV head]; k_scales and v_scales hold one fp32 number per tile in the same order.  A number is its code times the
+ * scale of its tile:
+ *   CQ_Q8_INT8   an integer c from -127 to 127, stored as the byte c + 128; scale = largest magnitude / 127
+ *   CQ_Q8_E4M3   an OCP e4m3 number; scale = the smallest power of two at which the largest magnitude is at most 448, so that a
+ *                scale that grows later moves codes without rounding them again (but for the smallest)
+ * Integers are the more exact where a block's numbers are of one size, e4m3 where they span many.
+ *
+ * All *_q8 calls name tokens alike: sequence n has t_n = seq_lens[n] tokens (default t; values are clamped into [0, t]), and
+ * row j of a call with m rows per sequence sits at position t_n - m + j.  Rows in front of position 0 are padding: they
+ * are not read where they are inputs and left as they are where they are outputs, but for attention, whose padding rows become zero.
+ *
+ * cq_append_q8[_paged]   writes the last m tokens of every sequence.
+ *   x_k, x_v          device, fp16 [batch][m][n_kv_heads][128] as a projection leaves them; element strides x_batch_stride and x_row_stride
+ *                     (>= n_kv_heads * 128) as in cq_encode_kv
+ *   t                 tokens of a sequence including the new ones, m <= t <= t_cap
+ *   rope_table        device, as written by cq_q8_rope_table, or NULL: keys are stored as they are.  With a table they are rotated
+ *                     to their positions first (the rotation of cq_rope_table's calls); rope_positions >= t then, else 0
+ *   q                 device, fp16 [batch][m][n_q_heads][128] by element strides q_batch_stride, q_row_stride, or NULL: no queries
+ *                     (needs a table).  Rotated to the same positions in the same launch, rounded once
+ *   q_out             device, fp16 [batch][m][n_q_heads][128]; may be q itself where q has no gaps
+ *   A block that holds older tokens keeps its scale or takes the larger one that the new tokens need; older codes then become
+ *   the nearest ones under it.  A block that begins with a new token takes the scale of its new tokens, whatever it held.  What
+ *   lies behind t_n is left as it is, and sequences may be cut back (a smaller t_n) at any time.  Codes, nearest with ties to
+ *   even, and scales are those of exact arithmetic (the kernel computes in fp64), but for numbers within 2^-45 of a border.
+ *   Equal calls give equal bits; how a prompt is cut into calls changes only codes of blocks that a cut runs through.
+ *   Two sequences must not share a page that is written.  Inputs must be finite.
+ * cq_q8_rope_table       fills the table of cq_append_q8: fp64 cosines and sines, cq_q8_rope_table_bytes(head_dim, positions) bytes,
+ *                     written asynchronously; arguments as cq_rope_table.
+ * cq_dequantize_q8[_paged]   the last m tokens of every sequence as fp16 rows (code times scale, rounded to nearest; a rotated
+ *                     key beyond fp16's range becomes infinite).  k_out or v_out may be NULL: not wanted
+ *   k_out, v_out      device, fp16 [batch][m][n_kv_heads * 128] by element strides (multiples of 8)
+ * cq_decode_attention_q8[_paged]   Eq. 1 for one query token per sequence at position t_n - 1 (t_n = 0: a row of zeros).
+ *   q, out            device, fp16 [batch][n_q_heads][128]; query head h reads KV head h / (n_q_heads / n_kv_heads)
+ * cq_chunk_attention_q8[_paged]    the same for the last m tokens of every sequence, causally.
+ *   q, out            device, fp16 [batch][m][n_q_heads][128]
+ *   tokens_per_split  0 = the library's choice; otherwise a multiple of 64: the context is cut into pieces of this many tokens
+ *   workspace         device, cq_attention_q8_workspace_bytes(...) bytes (decode: m = 1)
+ *   Products on the matrix cores: codes (exact in fp16) by fp16 queries, summed in fp32; scores, softmax and sums in fp32;
+ *   each weight is rounded to fp16 once (relative to the largest so far, of which it may be 2^-38) where it meets the
+ *   values' codes; the result is rounded to fp16.  Sizes alone choose the kernel and the pieces; no atomics on
+ *   results: equal calls give equal bits.  Scores must be finite in fp32.
+ * Formats: head_dim 128.  Errors: as cq_decode_attention and cq_encode_kv; CQ_ERR_INVALID_ARG also for an unknown kind, arrays that
+ * overlap where one is written, q without a table, and a table that ends before t.
+ */
+#define CQ_Q8_INT8 1
+#define CQ_Q8_E4M3 2
+
+typedef struct cq_q8_format {
+    int32_t kind;         /* CQ_Q8_INT8 or CQ_Q8_E4M3 */
+    int32_t head_dim;     /* 128 */
+    int32_t n_kv_heads;
+} cq_q8_format;
+
+typedef struct cq_q8_cache {
+    void *k_codes, *v_codes;       /* device, cq_q8_cache_bytes(...) (cq_q8_paged_cache_bytes) bytes each */
+    float *k_scales, *v_scales;    /* device, one per 8192 bytes of codes */
+} cq_q8_cache;
+
+/* Code bytes of one cache (K or V of one layer), or of a pool of n_pages pages.  0 on bad arguments. */
+CQ_API size_t cq_q8_cache_bytes(const cq_q8_format *fmt, int32_t batch, int32_t t_cap);
+CQ_API size_t cq_q8_paged_cache_bytes(const cq_q8_format *fmt, int32_t n_pages);
+CQ_API size_t cq_q8_rope_table_bytes(int32_t head_dim, int32_t positions);
+CQ_API cq_status cq_q8_rope_table(double base, int32_t head_dim, int32_t positions, void *table, size_t table_bytes, void *stream);
+CQ_API cq_status cq_append_q8(const void *x_k, const void *x_v, int64_t x_batch_stride, int64_t x_row_stride, const cq_q8_cache *cache,
+                       const cq_q8_format *fmt, int32_t batch, int32_t m, int32_t t, int32_t t_cap, const int32_t *seq_lens,
+                       const void *rope_table, int32_t rope_positions,
+                       const void *q, int64_t q_batch_stride, int64_t q_row_stride, int32_t n_q_heads, void *q_out, void *stream);
+CQ_API cq_status cq_append_q8_paged(const void *x_k, const void *x_v, int64_t x_batch_stride, int64_t x_row_stride, const cq_q8_cache *cache,
+                             const cq_q8_format *fmt, int32_t batch, int32_t m, int32_t t, const cq_page_table *pages, const int32_t *seq_lens,
+                             const void *rope_table, int32_t rope_positions,
+                             const void *q, int64_t q_batch_stride, int64_t q_row_stride, int32_t n_q_heads, void *q_out, void *stream);
+CQ_API cq_status cq_dequantize_q8(const cq_q8_cache *cache, const cq_q8_format *fmt, int32_t batch, int32_t m, int32_t t, int32_t t_cap,
+                           const int32_t *seq_lens, void *k_out, void *v_out, int64_t out_batch_stride, int64_t out_row_stride, void *stream);
+CQ_API cq_status cq_dequantize_q8_paged(const cq_q8_cache *cache, const cq_q8_format *fmt, int32_t batch, int32_t m, int32_t t,
+                                 const cq_page_table *pages, const int32_t *seq_lens,
+                                 void *k_out, void *v_out, int64_t out_batch_stride, int64_t out_row_stride, void *stream);
+/* Tokens per piece of the context that the library would choose, and the workspace of such a call (never 0 for good arguments). */
+CQ_API int32_t cq_attention_q8_default_split(const cq_q8_format *fmt, int32_t batch, int32_t n_q_heads, int32_t m, int32_t t);
+CQ_API size_t cq_attention_q8_workspace_bytes(const cq_q8_format *fmt, int32_t batch, int32_t n_q_heads, int32_t m, int32_t t,
+                                       int32_t tokens_per_split);
+CQ_API cq_status cq_decode_attention_q8(const void *q, const cq_q8_cache *cache, float scale, const cq_q8_format *fmt,
+                                 int32_t batch, int32_t n_q_heads, int32_t t, int32_t t_cap, const int32_t *seq_lens, int32_t tokens_per_split,
+                                 void *out, void *workspace, size_t workspace_bytes, void *stream);
+CQ_API cq_status cq_decode_attention_q8_paged(const void *q, const cq_q8_cache *cache, float scale, const cq_q8_format *fmt,
+                                       int32_t batch, int32_t n_q_heads, int32_t t, const cq_page_table *pages, const int32_t *seq_lens,
+                                       int32_t tokens_per_split, void *out, void *workspace, size_t workspace_bytes, void *stream);
+CQ_API cq_status cq_chunk_attention_q8(const void *q, const cq_q8_cache *cache, float scale, const cq_q8_format *fmt,
+                                int32_t batch, int32_t n_q_heads, int32_t m, int32_t t, int32_t t_cap, const int32_t *seq_lens,
+                                int32_t tokens_per_split, void *out, void *workspace, size_t workspace_bytes, void *stream);
+CQ_API cq_status cq_chunk_attention_q8_paged(const void *q, const cq_q8_cache *cache, float scale, const cq_q8_format *fmt,
+                                      int32_t batch, int32_t n_q_heads, int32_t m, int32_t t, const cq_page_table *pages, const int32_t *seq_lens,
+                                      int32_t tokens_per_split, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * cq_dequantize -- the inverse lookup ("dequantization", Section 2.2; CQ(A) of Eq. 5 as values):
  * out[n][t][g c + i] = centroids[g][code(n, t_offset + t, g)][i] for t = 0 .. t_count - 1, bit
  * for bit the stored fp16 centroids.  For callers that need dense keys / values (e.g. a

@@ -41,6 +41,9 @@ EXPORTS = (
     "cq_decode_weights_workspace_bytes", "cq_decode_attention_weights", "cq_decode_attention_weights_paged",
     "cq_chunk_weights_workspace_bytes", "cq_chunk_weights", "cq_chunk_weights_paged",
     "cq_select_workspace_bytes", "cq_select_tokens", "cq_compact_workspace_bytes", "cq_compact_cache", "cq_compact_cache_paged",
+    "cq_q8_cache_bytes", "cq_q8_paged_cache_bytes", "cq_q8_rope_table_bytes", "cq_q8_rope_table", "cq_append_q8", "cq_append_q8_paged",
+    "cq_dequantize_q8", "cq_dequantize_q8_paged", "cq_attention_q8_default_split", "cq_attention_q8_workspace_bytes",
+    "cq_decode_attention_q8", "cq_decode_attention_q8_paged", "cq_chunk_attention_q8", "cq_chunk_attention_q8_paged",
     "cq_probe_stream_read", "cq_probe_copy", "cq_probe_mfma", "cq_probe_decode_plan",
 )
 
@@ -64,6 +67,14 @@ class _LayerIO(ctypes.Structure):
 class _PageTable(ctypes.Structure):
     _fields_ = [("n_pages", ctypes.c_int32), ("max_tiles", ctypes.c_int32), ("row_stride", ctypes.c_int64),
                 ("block_table", ctypes.c_void_p)]
+
+
+class _Q8Format(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32)]
+
+
+class _Q8Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "v_codes", "k_scales", "v_scales")]
 
 
 @dataclass(frozen=True)
@@ -231,6 +242,22 @@ def load() -> ctypes.CDLL:
     for at, name in ((i32, "cq_compact_cache"), (pp, "cq_compact_cache_paged")):
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = [vp, vp, vp, i64, fp, i32, i32, at, vp, vp, i32, vp, vp, vp, i64, at, vp, size, vp]
+    qf, qc = ctypes.POINTER(_Q8Format), ctypes.POINTER(_Q8Cache)
+    for name, args in (("cq_q8_cache_bytes", [qf, i32, i32]), ("cq_q8_paged_cache_bytes", [qf, i32]), ("cq_q8_rope_table_bytes", [i32, i32]),
+                       ("cq_attention_q8_workspace_bytes", [qf, i32, i32, i32, i32, i32])):
+        getattr(lib, name).restype = size
+        getattr(lib, name).argtypes = args
+    lib.cq_attention_q8_default_split.restype = i32
+    lib.cq_attention_q8_default_split.argtypes = [qf, i32, i32, i32, i32]
+    lib.cq_q8_rope_table.restype = ctypes.c_int
+    lib.cq_q8_rope_table.argtypes = [ctypes.c_double, i32, i32, vp, size, vp]
+    for at, paged in ((i32, ""), (pp, "_paged")):
+        for name, args in (("cq_append_q8", [vp, vp, i64, i64, qc, qf, i32, i32, i32, at, vp, vp, i32, vp, i64, i64, i32, vp, vp]),
+                           ("cq_dequantize_q8", [qc, qf, i32, i32, i32, at, vp, vp, vp, i64, i64, vp]),
+                           ("cq_decode_attention_q8", [vp, qc, f32, qf, i32, i32, i32, at, vp, i32, vp, vp, size, vp]),
+                           ("cq_chunk_attention_q8", [vp, qc, f32, qf, i32, i32, i32, i32, at, vp, i32, vp, vp, size, vp])):
+            getattr(lib, name + paged).restype = ctypes.c_int
+            getattr(lib, name + paged).argtypes = args
     lib.cq_probe_copy.restype = ctypes.c_int
     lib.cq_probe_copy.argtypes = [vp, vp, ctypes.c_size_t, vp]
     lib.cq_probe_mfma.restype = ctypes.c_int
@@ -289,8 +316,10 @@ def _tensors(x):
         yield x
     elif isinstance(x, PageTable):
         yield x.block_table
-    elif isinstance(x, RopeTable):
+    elif isinstance(x, (RopeTable, Q8RopeTable)):
         yield x.table
+    elif isinstance(x, Q8Cache):
+        yield from (x.k, x.v, x.k_scales, x.v_scales)
     elif isinstance(x, LayerTable):
         yield x.table
         yield from _tensors(x._keep)
@@ -1563,3 +1592,258 @@ def cq_compact_cache_paged(k_pool, v_pool, weights, fmt: CQFormat, kept, kept_le
     """cq_compact_cache from the pages of `pages` to those of `pages_out` (default: in place)."""
     _run(stream, prepare_compact_cache, k_pool, v_pool, weights, fmt, kept, kept_lens, t, 0, k_pool_out, v_pool_out,
          weights_out, 0, pages, pages_out, workspace)
+
+
+# ---------------------------------------------------------------- the 8-bit block cache
+
+Q8_KINDS = {"int8": 1, "e4m3": 2}
+
+
+@dataclass(frozen=True)
+class Q8Format:
+    """The 8-bit block cache on ``n_kv_heads`` heads of ``head_dim`` channels: "int8" or "e4m3" codes, a scale for each
+    block of 64 tokens and head."""
+    kind: str
+    head_dim: int
+    n_kv_heads: int
+
+    def _c(self) -> _Q8Format:
+        if self.kind not in Q8_KINDS:
+            raise ValueError(f"kind must be one of {tuple(Q8_KINDS)}, got {self.kind!r}")
+        return _Q8Format(Q8_KINDS[self.kind], self.head_dim, self.n_kv_heads)
+
+    @property
+    def channels(self) -> int:
+        return self.head_dim * self.n_kv_heads
+
+
+@dataclass(frozen=True)
+class Q8Cache:
+    """The arrays of an 8-bit block cache, or of its pools: uint8 codes of keys and values, and fp32 scales, one for each
+    8192 bytes of codes."""
+    k: "torch.Tensor"
+    v: "torch.Tensor"
+    k_scales: "torch.Tensor"
+    v_scales: "torch.Tensor"
+
+    def _c(self) -> _Q8Cache:
+        return _Q8Cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scales.data_ptr(), self.v_scales.data_ptr())
+
+
+def cq_q8_cache_bytes(fmt: Q8Format, batch: int, t_cap: int) -> int:
+    return int(load().cq_q8_cache_bytes(ctypes.byref(fmt._c()), batch, t_cap))
+
+
+def cq_q8_paged_cache_bytes(fmt: Q8Format, n_pages: int) -> int:
+    return int(load().cq_q8_paged_cache_bytes(ctypes.byref(fmt._c()), n_pages))
+
+
+def cq_attention_q8_default_split(fmt: Q8Format, batch: int, n_q_heads: int, m: int, t: int) -> int:
+    return int(load().cq_attention_q8_default_split(ctypes.byref(fmt._c()), batch, n_q_heads, m, t))
+
+
+def cq_attention_q8_workspace_bytes(fmt: Q8Format, batch: int, n_q_heads: int, m: int, t: int, tokens_per_split: int = 0) -> int:
+    return int(load().cq_attention_q8_workspace_bytes(ctypes.byref(fmt._c()), batch, n_q_heads, m, t, tokens_per_split))
+
+
+def _q8_arrays(nbytes: int, what: str, device) -> Q8Cache:
+    import torch
+    if nbytes == 0:
+        raise CQError(CQ_ERR_INVALID_ARG, what)
+    codes = [torch.empty(nbytes, dtype=torch.uint8, device=device) for _ in range(2)]
+    return Q8Cache(*codes, *(torch.empty(nbytes // 8192, dtype=torch.float32, device=device) for _ in range(2)))
+
+
+def alloc_q8_cache(fmt: Q8Format, batch: int, t_cap: int, device="cuda") -> Q8Cache:
+    """Device arrays of a contiguous 8-bit block cache (uninitialised)."""
+    return _q8_arrays(cq_q8_cache_bytes(fmt, batch, t_cap), "cq_q8_cache_bytes", device)
+
+
+def alloc_q8_pools(fmt: Q8Format, n_pages: int, device="cuda") -> Q8Cache:
+    """Device arrays of the pools of a paged 8-bit block cache (uninitialised)."""
+    return _q8_arrays(cq_q8_paged_cache_bytes(fmt, n_pages), "cq_q8_paged_cache_bytes", device)
+
+
+class Q8RopeTable:
+    """The trigonometric table of cq_q8_rope_table (fp64) on the device: covers positions [0, positions)."""
+
+    @_on_stream
+    def __init__(self, base: float, positions: int, head_dim: int = 128, device="cuda", stream=None):
+        import torch
+        nbytes = int(load().cq_q8_rope_table_bytes(head_dim, positions))
+        if nbytes == 0:
+            raise CQError(CQ_ERR_INVALID_ARG, "cq_q8_rope_table_bytes")
+        self.base, self.positions, self.head_dim = float(base), int(positions), int(head_dim)
+        self.table = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        _same_device(self.table)
+        st = load().cq_q8_rope_table(self.base, head_dim, positions, self.table.data_ptr(), nbytes, _stream_handle(stream))
+        if st != CQ_OK:
+            raise CQError(st, "cq_q8_rope_table")
+
+
+def _check_q8(cache: Q8Cache, fmt: Q8Format, batch: int, t_cap: int, pages, seq_lens):
+    """The checks that all q8 calls share; returns (format, cache, capacity or page table, seq_lens pointer) for the C ABI."""
+    import torch
+    need = cq_q8_paged_cache_bytes(fmt, pages.n_pages) if pages is not None else cq_q8_cache_bytes(fmt, batch, t_cap)
+    if need == 0:
+        raise CQError(CQ_ERR_INVALID_ARG, "cq_q8_cache_bytes")
+    for x, dtype, size, what in ((cache.k, torch.uint8, need, "k"), (cache.v, torch.uint8, need, "v"),
+                                 (cache.k_scales, torch.float32, need // 8192, "k_scales"), (cache.v_scales, torch.float32, need // 8192, "v_scales")):
+        _dev(x, dtype, what)
+        if not x.is_contiguous() or x.numel() < size:
+            raise ValueError(f"{what} must be contiguous and as large as the format, batch and capacity need")
+    if pages is not None and pages.block_table.shape[0] < batch:
+        raise ValueError("block table has fewer rows than the batch")
+    sl = _check_seq_lens(seq_lens, batch)
+    _same_device(cache.k, cache.v, cache.k_scales, cache.v_scales, seq_lens, None if pages is None else pages.block_table)
+    return fmt._c(), cache._c(), t_cap if pages is None else ctypes.byref(pages._c), sl
+
+
+def _strides(x, width: int) -> tuple:
+    """Batch and row stride of [B, m, ...] rows of `width` elements (those of a dimension of size 1 mean nothing)."""
+    row = int(x.stride(1)) if x.shape[1] > 1 else width
+    return (int(x.stride(0)) if x.shape[0] > 1 else 0), row
+
+
+def prepare_append_q8(x_k, x_v, cache: Q8Cache, fmt: Q8Format, t: int, t_cap: int = 0, pages=None, seq_lens=None, rope=None,
+                      q=None, q_out=None):
+    """Check and marshal the arguments of cq_append_q8 (or, with `pages`, of its paged form) once.  Returns (call, q_out)."""
+    import torch
+    for what, x in (("x_k", x_k), ("x_v", x_v)):
+        _dev(x, torch.float16, what)
+        if x.dim() != 3 or x.stride(2) != 1 or x.shape[2] != fmt.channels:
+            raise ValueError(f"{what} must be [B, m, n_kv_heads * head_dim] with unit channel stride")
+    batch, m = int(x_k.shape[0]), int(x_k.shape[1])
+    if x_v.shape != x_k.shape or _strides(x_v, fmt.channels) != _strides(x_k, fmt.channels):
+        raise ValueError("x_k and x_v must have the same shape and strides")
+    f, c, at, sl = _check_q8(cache, fmt, batch, t_cap, pages, seq_lens)
+    if rope is not None and not isinstance(rope, Q8RopeTable):
+        raise TypeError("rope must be a Q8RopeTable")
+    queries = (None, 0, 0, 0, None)
+    if q is not None:
+        _dev(q, torch.float16, "q")
+        if q.dim() != 4 or tuple(q.shape[:2]) != (batch, m) or q.shape[3] != fmt.head_dim or q.stride(3) != 1 or (q.shape[2] > 1 and q.stride(2) != fmt.head_dim):
+            raise ValueError("q must be [B, m, Hq, head_dim] with its heads side by side")
+        hq = int(q.shape[2])
+        q_out = _check_out(q_out, (batch, m, hq, fmt.head_dim), q.device)
+        queries = (q.data_ptr(), *_strides(q, hq * fmt.head_dim), hq, q_out.data_ptr())
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _same_device(x_k, x_v, q, q_out, None if rope is None else rope.table)
+    args = (x_k.data_ptr(), x_v.data_ptr(), *_strides(x_k, fmt.channels), ctypes.byref(c), ctypes.byref(f), batch, m, t, at, sl,
+            None if rope is None else rope.table.data_ptr(), 0 if rope is None else rope.positions, *queries)
+    name = "cq_append_q8" if pages is None else "cq_append_q8_paged"
+    return PreparedCall(getattr(load(), name), args, (x_k, x_v, cache, f, c, pages, seq_lens, rope, q, q_out), name), q_out
+
+
+@_on_stream
+def cq_append_q8(x_k, x_v, cache: Q8Cache, fmt: Q8Format, t: int, t_cap: int, seq_lens=None, rope=None, q=None, q_out=None, stream=None):
+    """Append the last m tokens of every sequence to an 8-bit block cache: x_k, x_v fp16 [B, m, n_kv_heads * head_dim] (strided),
+    token j of sequence n at position seq_lens[n] - m + j (default t - m + j; padding in front of 0).  With `rope`, keys are rotated to
+    their positions, and queries `q` [B, m, Hq, head_dim] too, into q_out, which is returned."""
+    return _run(stream, prepare_append_q8, x_k, x_v, cache, fmt, t, t_cap, None, seq_lens, rope, q, q_out)[0]
+
+
+@_on_stream
+def cq_append_q8_paged(x_k, x_v, cache: Q8Cache, fmt: Q8Format, t: int, pages: PageTable, seq_lens=None, rope=None, q=None, q_out=None,
+                       stream=None):
+    """cq_append_q8 into paged pools."""
+    return _run(stream, prepare_append_q8, x_k, x_v, cache, fmt, t, 0, pages, seq_lens, rope, q, q_out)[0]
+
+
+def prepare_dequantize_q8(cache: Q8Cache, fmt: Q8Format, batch: int, m: int, t: int, k_out=None, v_out=None, t_cap: int = 0, pages=None,
+                          seq_lens=None):
+    """Check and marshal the arguments of cq_dequantize_q8 (or of its paged form) once.  Returns (call, k_out, v_out)."""
+    import torch
+    f, c, at, sl = _check_q8(cache, fmt, batch, t_cap, pages, seq_lens)
+    if k_out is None and v_out is None:
+        k_out, v_out = (torch.empty((batch, m, fmt.channels), dtype=torch.float16, device=cache.k.device) for _ in range(2))
+    outs = [x for x in (k_out, v_out) if x is not None]
+    for x in outs:
+        _dev(x, torch.float16, "out")
+        if tuple(x.shape) != (batch, m, fmt.channels) or x.stride(2) != 1:
+            raise ValueError("outputs must be [B, m, n_kv_heads * head_dim] with unit channel stride")
+    if _strides(outs[0], fmt.channels) != _strides(outs[-1], fmt.channels):
+        raise ValueError("outputs must have the same strides")
+    _same_device(*outs)
+    args = (ctypes.byref(c), ctypes.byref(f), batch, m, t, at, sl, *(None if x is None else x.data_ptr() for x in (k_out, v_out)),
+            *_strides(outs[0], fmt.channels))
+    name = "cq_dequantize_q8" if pages is None else "cq_dequantize_q8_paged"
+    return PreparedCall(getattr(load(), name), args, (cache, f, c, pages, seq_lens, k_out, v_out), name), k_out, v_out
+
+
+@_on_stream
+def cq_dequantize_q8(cache: Q8Cache, fmt: Q8Format, batch: int, m: int, t: int, t_cap: int, seq_lens=None, k_out=None, v_out=None,
+                     stream=None) -> tuple:
+    """(keys, values) of the last m tokens of every sequence, fp16 [B, m, n_kv_heads * head_dim]; with one output given, only that
+    one.  Rows in front of position 0 are left as they are."""
+    return _run(stream, prepare_dequantize_q8, cache, fmt, batch, m, t, k_out, v_out, t_cap, None, seq_lens)
+
+
+@_on_stream
+def cq_dequantize_q8_paged(cache: Q8Cache, fmt: Q8Format, batch: int, m: int, t: int, pages: PageTable, seq_lens=None, k_out=None,
+                           v_out=None, stream=None) -> tuple:
+    """cq_dequantize_q8 from paged pools."""
+    return _run(stream, prepare_dequantize_q8, cache, fmt, batch, m, t, k_out, v_out, 0, pages, seq_lens)
+
+
+def _prepare_attention_q8(name: str, q, cache: Q8Cache, scale: float, fmt: Q8Format, t: int, t_cap: int, pages, seq_lens,
+                          tokens_per_split: int, out, workspace):
+    import torch
+    _dev(q, torch.float16, "q")
+    chunk = name == "cq_chunk_attention_q8"
+    if q.dim() != 3 + chunk or not q.is_contiguous() or q.shape[-1] != fmt.head_dim:
+        raise ValueError(f"q must be contiguous {'[B, m, Hq, head_dim]' if chunk else '[B, Hq, head_dim]'}")
+    batch, m, hq = int(q.shape[0]), int(q.shape[1]) if chunk else 1, int(q.shape[-2])
+    f, c, at, sl = _check_q8(cache, fmt, batch, t_cap, pages, seq_lens)
+    out = _check_out(out, q.shape, q.device)
+    workspace = _workspace(workspace, cq_attention_q8_workspace_bytes(fmt, batch, hq, m, t, tokens_per_split), q.device,
+                           "cq_attention_q8_workspace_bytes")
+    _same_device(q, out, workspace)
+    args = (q.data_ptr(), ctypes.byref(c), float(scale), ctypes.byref(f), batch, hq, *((m,) if chunk else ()), t, at, sl, tokens_per_split,
+            out.data_ptr(), workspace.data_ptr(), workspace.numel())
+    name += "" if pages is None else "_paged"
+    return PreparedCall(getattr(load(), name), args, (q, cache, f, c, pages, seq_lens, out, workspace), name), out
+
+
+def prepare_decode_attention_q8(q, cache: Q8Cache, scale: float, fmt: Q8Format, t: int, t_cap: int = 0, pages=None, seq_lens=None,
+                                tokens_per_split: int = 0, out=None, workspace=None):
+    """Check and marshal the arguments of cq_decode_attention_q8 (or of its paged form) once.  q fp16 [B, Hq, head_dim].  Returns
+    (call, out)."""
+    return _prepare_attention_q8("cq_decode_attention_q8", q, cache, scale, fmt, t, t_cap, pages, seq_lens, tokens_per_split, out, workspace)
+
+
+def prepare_chunk_attention_q8(q, cache: Q8Cache, scale: float, fmt: Q8Format, t: int, t_cap: int = 0, pages=None, seq_lens=None,
+                               tokens_per_split: int = 0, out=None, workspace=None):
+    """Check and marshal the arguments of cq_chunk_attention_q8 (or of its paged form) once.  q fp16 [B, m, Hq, head_dim].  Returns
+    (call, out)."""
+    return _prepare_attention_q8("cq_chunk_attention_q8", q, cache, scale, fmt, t, t_cap, pages, seq_lens, tokens_per_split, out, workspace)
+
+
+@_on_stream
+def cq_decode_attention_q8(q, cache: Q8Cache, scale: float, fmt: Q8Format, t: int, t_cap: int, seq_lens=None, tokens_per_split: int = 0,
+                           out=None, workspace=None, stream=None):
+    """Attention of one query token per sequence, q fp16 [B, Hq, head_dim], over an 8-bit block cache."""
+    return _run(stream, prepare_decode_attention_q8, q, cache, scale, fmt, t, t_cap, None, seq_lens, tokens_per_split, out, workspace)[0]
+
+
+@_on_stream
+def cq_decode_attention_q8_paged(q, cache: Q8Cache, scale: float, fmt: Q8Format, t: int, pages: PageTable, seq_lens=None,
+                                 tokens_per_split: int = 0, out=None, workspace=None, stream=None):
+    """cq_decode_attention_q8 over paged pools."""
+    return _run(stream, prepare_decode_attention_q8, q, cache, scale, fmt, t, 0, pages, seq_lens, tokens_per_split, out, workspace)[0]
+
+
+@_on_stream
+def cq_chunk_attention_q8(q, cache: Q8Cache, scale: float, fmt: Q8Format, t: int, t_cap: int, seq_lens=None, tokens_per_split: int = 0,
+                          out=None, workspace=None, stream=None):
+    """Causal attention of the last m tokens of every sequence, q fp16 [B, m, Hq, head_dim], over an 8-bit block cache; rows in front of
+    position 0 become zero."""
+    return _run(stream, prepare_chunk_attention_q8, q, cache, scale, fmt, t, t_cap, None, seq_lens, tokens_per_split, out, workspace)[0]
+
+
+@_on_stream
+def cq_chunk_attention_q8_paged(q, cache: Q8Cache, scale: float, fmt: Q8Format, t: int, pages: PageTable, seq_lens=None,
+                                tokens_per_split: int = 0, out=None, workspace=None, stream=None):
+    """cq_chunk_attention_q8 over paged pools."""
+    return _run(stream, prepare_chunk_attention_q8, q, cache, scale, fmt, t, 0, pages, seq_lens, tokens_per_split, out, workspace)[0]
