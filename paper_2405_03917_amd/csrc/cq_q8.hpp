@@ -66,6 +66,9 @@ struct Q8Plan {
     int tiles_per_split, n_split;
 };
 Q8Plan q8_plan(int batch, int n_kv_heads, int n_q_heads, int m, int t, int tokens_per_split);
+// Many rows per KV head (cq_q8_chunk.hip): kQ8ChunkRows of them to a workgroup.
+constexpr int kQ8ChunkRows = 128;
+cq_status launch_chunk_q8(const Q8AttentionArgs& a, int kind, hipStream_t stream);
 cq_status launch_attention_q8(const Q8AttentionArgs& a, int kind, const Q8Plan& plan, hipStream_t stream);
 
 #if defined(__HIP_DEVICE_COMPILE__) || defined(__HIPCC__)
@@ -95,6 +98,23 @@ __device__ __forceinline__ q8_half8 q8_half8_of(unsigned w0, unsigned w1)
     q8_halves<KIND>(w0, &a, &b);
     q8_halves<KIND>(w1, &c, &d);
     return q8_half8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+constexpr float kQ8Lowest = -3.402823466e38f;
+// Weights are 2^(score - reference + kQ8Above) with a reference that the largest score may pass by kQ8Slack before it is moved: at most
+// 2^15 in fp16, and those of 2^-14 of fp16's normal numbers are 2^-21 of the largest, its smallest 2^-31.
+constexpr float kQ8Slack = 8.f, kQ8Above = 7.f;
+
+// The bytes of tokens that are not there (from `from` on, of 16 in order) become zero: an e4m3 byte may be no number, and its
+// weight of zero would not hide it.
+__device__ __forceinline__ q8_u4 q8_only_before(q8_u4 w, int from)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int keep = from - 4 * i;
+        w[i] = keep >= 4 ? w[i] : keep <= 0 ? 0u : w[i] & (0xffffffffu >> (32 - 8 * keep));
+    }
+    return w;
 }
 #endif
 

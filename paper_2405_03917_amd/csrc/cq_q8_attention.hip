@@ -17,15 +17,10 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
-constexpr float kLowest = -3.402823466e38f;
-// Weights are 2^(score - reference + kAbove) with a reference that the largest score may pass by kSlack before it is moved: at most
-// 2^15 in fp16, and those of 2^-14 of fp16's normal numbers are 2^-21 of the largest, its smallest 2^-31.
-constexpr float kSlack = 8.f, kAbove = 7.f;
-
 // One row's weighted values from its pieces: `n` of (reference, sum, 128 channels), `stride` floats apart; channel i.
 __device__ __forceinline__ float merged(const float* p, int n, size_t stride, int i)
 {
-    float m = kLowest, l = 0.f, o = 0.f;
+    float m = kQ8Lowest, l = 0.f, o = 0.f;
 #pragma unroll 4
     for (int s = 0; s < n; ++s) {
         const float ms = p[s * stride], ls = p[s * stride + 1], os = p[s * stride + kPartialHeader + i];
@@ -46,18 +41,6 @@ __global__ __launch_bounds__(kThreads) void merge_q8_kernel(const float* partial
     if (row >= rows) return;
     const _Float16 h = (_Float16)merged(partials + row * n_split * kQ8Partial, n_split, kQ8Partial, i);
     out[row * kQ8Head + i] = __builtin_bit_cast(uint16_t, h);
-}
-
-// The bytes of tokens that are not there (from `from` on, of 16 in order) become zero: an e4m3 byte may be no number, and its
-// weight of zero would not hide it.
-__device__ __forceinline__ q8_u4 only_before(q8_u4 w, int from)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int keep = from - 4 * i;
-        w[i] = keep >= 4 ? w[i] : keep <= 0 ? 0u : w[i] & (0xffffffffu >> (32 - 8 * keep));
-    }
-    return w;
 }
 
 template <int KIND, int RB>
@@ -97,7 +80,7 @@ __global__ __launch_bounds__(kThreads) void rows_q8_kernel(Q8AttentionArgs a, in
     float ref[RB], sum[RB];
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-        ref[r] = kLowest;
+        ref[r] = kQ8Lowest;
         sum[r] = 0.f;
 #pragma unroll
         for (int c = 0; c < 8; ++c) o[r][c] = q8_float4{0.f, 0.f, 0.f, 0.f};
@@ -162,7 +145,7 @@ __global__ __launch_bounds__(kThreads) void rows_q8_kernel(Q8AttentionArgs a, in
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, x[i]);
-            if (__any(top > ref[r] + kSlack)) {
+            if (__any(top > ref[r] + kQ8Slack)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
                 const float now = fmaxf(ref[r], top), keep = __builtin_amdgcn_exp2f(ref[r] - now);
@@ -171,7 +154,7 @@ __global__ __launch_bounds__(kThreads) void rows_q8_kernel(Q8AttentionArgs a, in
 #pragma unroll
                 for (int c = 0; c < 8; ++c) o[r][c] *= keep;
             }
-            const float below = ref[r] - kAbove;
+            const float below = ref[r] - kQ8Above;
             float w[16], part = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -186,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void rows_q8_kernel(Q8AttentionArgs a, in
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
             q8_u4 w = vr[c];
-            if (cut) w = only_before(w, t_n - first);
+            if (cut) w = q8_only_before(w, t_n - first);
             const q8_half8 v0 = q8_half8_of<KIND>(w[0], w[1]), v1 = q8_half8_of<KIND>(w[2], w[3]);
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
@@ -222,7 +205,7 @@ __global__ __launch_bounds__(kThreads) void rows_q8_kernel(Q8AttentionArgs a, in
         if (row >= rows) continue;
         const int j = row / qper;
         const size_t at = ((size_t)n * a.m + j) * a.n_q_heads + h * qper + (row - j * qper);
-        float m = kLowest, l = 0.f, y[8];
+        float m = kQ8Lowest, l = 0.f, y[8];
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) m = fmaxf(m, lds[w][local][0]);
 #pragma unroll
@@ -269,9 +252,13 @@ Q8Plan q8_plan(int batch, int n_kv_heads, int n_q_heads, int m, int t, int token
     const int64_t rows = (int64_t)m * (n_q_heads / n_kv_heads);
     const int n_tiles = (t - 1) / kTileTokens + 1;
     Q8Plan p;
-    p.row_block = rows <= 16 ? 16 : 32;
+    p.row_block = rows <= 16 ? 16 : rows <= 64 ? 32 : kQ8ChunkRows;
     if (tokens_per_split) {
         p.tiles_per_split = tokens_per_split / kTileTokens;
+    } else if (p.row_block == kQ8ChunkRows) {
+        const int64_t blocks = (int64_t)batch * n_kv_heads * ((rows + p.row_block - 1) / p.row_block);
+        const int64_t pieces = std::max<int64_t>(1, std::min<int64_t>((n_tiles + 7) / 8, 512 / blocks));
+        p.tiles_per_split = (int)((n_tiles + pieces - 1) / pieces);
     } else {
         const int64_t blocks = (int64_t)batch * n_kv_heads * ((rows + p.row_block - 1) / p.row_block);
         const int64_t pieces = std::max<int64_t>(1, std::min<int64_t>((n_tiles + kWaves - 1) / kWaves, 1024 / blocks));
@@ -285,7 +272,8 @@ Q8Plan q8_plan(int batch, int n_kv_heads, int n_q_heads, int m, int t, int token
 cq_status launch_attention_q8(const Q8AttentionArgs& a, int kind, const Q8Plan& plan, hipStream_t stream)
 {
     const int64_t rows = (int64_t)a.batch * a.m * a.n_q_heads, merges = (rows + kThreads / kQ8Head - 1) / (kThreads / kQ8Head);
-    const cq_status st = kind == CQ_Q8_INT8 ? launch_rows<CQ_Q8_INT8>(a, plan.row_block, stream) : launch_rows<CQ_Q8_E4M3>(a, plan.row_block, stream);
+    const cq_status st = plan.row_block == kQ8ChunkRows ? launch_chunk_q8(a, kind, stream)
+                         : kind == CQ_Q8_INT8 ? launch_rows<CQ_Q8_INT8>(a, plan.row_block, stream) : launch_rows<CQ_Q8_E4M3>(a, plan.row_block, stream);
     if (st != CQ_OK || a.n_split == 1) return st;
     hipLaunchKernelGGL(merge_q8_kernel, dim3((unsigned)merges), dim3(kThreads), 0, stream, a.partials, a.out, rows, a.n_split);
     return hipGetLastError() == hipSuccess ? CQ_OK : CQ_ERR_HIP;

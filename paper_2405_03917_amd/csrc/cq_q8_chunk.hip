@@ -1,0 +1,269 @@
+// Attention over the 8-bit block cache for many rows per KV head (cq_chunk_attention_q8), for gfx950.
+//
+// The products of cq_q8_attention.hip, with a tile's codes turned into fp16 once for a workgroup: its wavefronts share them through LDS
+// and each serve rows of their own.  A tile lies in LDS as the operands of the products, 16 bytes a lane one behind the
+// other, so that neither writing nor reading them meets a bank twice.  Two tiles' room: while one is worked off the next
+// is converted, and the one after that is on its way from memory.
+// Values keep their codes; a block's scale goes into its weights, relative to the largest scale so far (2^(score - reference) by
+// v_scale / v_largest, an addition to the exponent), and out of their sum again.
+#include <algorithm>
+
+#include "cq_q8.hpp"
+
+namespace cq {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * 64;
+constexpr float kFaintest = -60.f;                          // log2 of a scale relative to the largest, below which it makes no difference
+
+template <int KIND, int RB>
+__global__ __launch_bounds__(kThreads, 2) void chunk_q8_kernel(Q8AttentionArgs a, int row_blocks, unsigned units)
+{
+    constexpr int ROWS = 16 * RB;                           // of a wavefront
+    extern __shared__ q8_u4 lds[];                          // [2][keys, values][16 operands][64 lanes]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, g = lane >> 4;
+    // the row blocks of a piece of a stream run on one XCD, which shares what it reads; the longest first
+    const unsigned eighth = blockIdx.x >> 3;
+    const int block = row_blocks - 1 - (int)(eighth % row_blocks);
+    const unsigned unit = (eighth / row_blocks) * 8 + (blockIdx.x & 7);
+    if (unit >= units) return;
+    const int split = unit % a.n_split, stream = unit / a.n_split;
+    const int n = stream / a.n_kv_heads, h = stream % a.n_kv_heads;
+    const int qper = a.n_q_heads / a.n_kv_heads, rows = a.m * qper;
+    const int t_n = a.length(n), pos0 = t_n - a.m;
+    const int row0 = block * (ROWS * kWaves) + wave * ROWS;
+    const int block_last = pos0 + (min((block + 1) * (ROWS * kWaves), rows) - 1) / qper;
+    const int n_tiles = block_last < 0 ? 0 : block_last / kTileTokens + 1;
+    const int tile0 = split * a.tiles_per_split, tile1 = min(tile0 + a.tiles_per_split, n_tiles);
+    // (a wavefront behind the last row repeats it and stores nothing)
+    const int pos_first = pos0 + min(row0, rows - 1) / qper, pos_last = pos0 + (min(row0 + ROWS, rows) - 1) / qper;
+    const float scale = fabsf(a.scale_log2e);
+
+    int pos[RB];
+    q8_half8 q[RB][4];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const int row = min(row0 + 16 * r + col, rows - 1), j = row / qper;
+        pos[r] = pos0 + j;
+        const uint16_t* src = a.q + (((size_t)n * a.m + j) * a.n_q_heads + h * qper + (row - j * qper)) * kQ8Head;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            q[r][s] = *reinterpret_cast<const q8_half8*>(src + 64 * (s >> 1) + 16 * g + 8 * (s & 1));
+            if (a.scale_log2e < 0.f) q[r][s] = -q[r][s];
+        }
+    }
+    q8_float4 o[RB][8];
+    float ref[RB], sum[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        ref[r] = kQ8Lowest;
+        sum[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) o[r][c] = q8_float4{0.f, 0.f, 0.f, 0.f};
+    }
+    float largest = 0.f;                                    // of the values' scales so far
+
+    // ---- wavefront w brings the keys of b = w and the values of channel blocks 2 w, 2 w + 1 (as in cq_q8_attention.hip)
+    q8_u4 gk[2], gv[2];
+    float ks = 0.f, vs = 0.f, ks_next = 0.f, vs_next = 0.f;
+    const unsigned k_off = (16 * (col >> 2) + 4 * wave + (col & 3)) * kQ8Head + 16 * g, v_off = (32 * wave + col) * kTileTokens + 16 * g;
+    auto request = [&](size_t at) {
+        const uint8_t* k = a.cache.codes[0] + at * kQ8TileBytes;
+        const uint8_t* v = a.cache.codes[1] + at * kQ8TileBytes;
+        gk[0] = *reinterpret_cast<const q8_u4*>(k + k_off);
+        gk[1] = *reinterpret_cast<const q8_u4*>(k + k_off + 64);
+        gv[0] = *reinterpret_cast<const q8_u4*>(v + v_off);
+        gv[1] = *reinterpret_cast<const q8_u4*>(v + v_off + 16 * kTileTokens);
+    };
+    auto stage = [&](int tile, int buf) {
+        q8_u4* k = lds + buf * 2048 + 256 * wave + lane;
+        q8_u4* v = lds + buf * 2048 + 1024 + 256 * wave + lane;
+        if (KIND == CQ_Q8_E4M3 && (tile + 1) * kTileTokens > t_n) {
+            gv[0] = q8_only_before(gv[0], t_n - tile * kTileTokens - 16 * g);
+            gv[1] = q8_only_before(gv[1], t_n - tile * kTileTokens - 16 * g);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            k[128 * i] = __builtin_bit_cast(q8_u4, q8_half8_of<KIND>(gk[i][0], gk[i][1]));
+            k[128 * i + 64] = __builtin_bit_cast(q8_u4, q8_half8_of<KIND>(gk[i][2], gk[i][3]));
+            v[128 * i] = __builtin_bit_cast(q8_u4, q8_half8_of<KIND>(gv[i][0], gv[i][1]));
+            v[128 * i + 64] = __builtin_bit_cast(q8_u4, q8_half8_of<KIND>(gv[i][2], gv[i][3]));
+        }
+    };
+    size_t at = 0;
+    auto place = [&](int tile) { return a.cache.map.tile_index(n, h, min(tile, tile1 - 1)); };
+    if (tile0 < tile1) {
+        at = place(tile0);
+        request(at);
+        ks_next = a.cache.scales[0][at];
+        vs_next = a.cache.scales[1][at];
+        at = place(tile0 + 1);
+        stage(tile0, 0);
+        if (tile0 + 1 < tile1) request(at);
+    }
+    __syncthreads();
+    int buf = 0;
+#pragma unroll 1
+    for (int tile = tile0; tile < tile1; ++tile, buf ^= 1) {
+        ks = ks_next;
+        vs = vs_next;
+        if (tile + 1 < tile1) {
+            ks_next = a.cache.scales[0][at];
+            vs_next = a.cache.scales[1][at];
+            stage(tile + 1, buf ^ 1);
+            at = place(tile + 2);
+            if (tile + 2 < tile1) request(at);
+        }
+        if (tile * kTileTokens <= pos_last) {
+            const q8_u4* k = lds + buf * 2048 + lane;
+            q8_float4 s[RB][4];
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) s[r][b] = q8_float4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const q8_half8 w = __builtin_bit_cast(q8_half8, k[64 * (4 * b + e)]);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) s[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w, q[r][e], s[r][b], 0, 0, 0);
+                }
+            // (a factor of zero stands for one so small that every weight is 1: 0 times a masked -infinity is no number)
+            const float by = fmaxf(scale * ks, 1e-37f);
+            if (tile * kTileTokens + kTileTokens - 1 > pos_first) {
+                const int first = tile * kTileTokens + 16 * g;
+#pragma unroll
+                for (int r = 0; r < RB; ++r)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[r][i >> 2][i & 3] = first + i > pos[r] ? -INFINITY : s[r][i >> 2][i & 3];
+            }
+            float top[RB];
+            bool over = vs > largest;
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                float x = s[r][0][0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) x = fmaxf(x, s[r][i >> 2][i & 3]);
+                top[r] = x * by;
+                over |= top[r] > ref[r] + kQ8Slack;
+            }
+            if (__any(over)) {
+                const float v_keep = vs > largest ? largest / vs : 1.f;
+                largest = fmaxf(largest, vs);
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    top[r] = fmaxf(top[r], __shfl_xor(top[r], 16));
+                    top[r] = fmaxf(top[r], __shfl_xor(top[r], 32));
+                    const float now = top[r] > ref[r] + kQ8Slack ? top[r] : ref[r], keep = __builtin_amdgcn_exp2f(ref[r] - now);
+                    ref[r] = now;
+                    sum[r] *= keep;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) o[r][c] *= keep * v_keep;
+                }
+            }
+            const float ratio = largest > 0.f ? vs / largest : 0.f;
+            const float bias = fmaxf(__builtin_amdgcn_logf(ratio), kFaintest), back = __builtin_amdgcn_exp2f(-bias);
+            bool wide = false;
+#pragma unroll
+            for (int r = 0; r < RB; ++r) wide |= fabsf(ref[r]) > 0x1p20f;
+            q8_half8 p[RB][2];
+            if (__any(wide)) {
+                // scores beyond 2^20: as rounded products, in their maximum and here (a fused multiply-add's would differ)
+#pragma unroll
+                for (int r = 0; r < RB; ++r)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+#pragma clang fp contract(off)
+                        const float x = s[r][i >> 2][i & 3] * by;
+                        s[r][i >> 2][i & 3] = (x - ref[r]) + (kQ8Above + bias);
+                    }
+            } else {
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    const float below = kQ8Above + bias - ref[r];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[r][i >> 2][i & 3] = fmaf(s[r][i >> 2][i & 3], by, below);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                float part = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(s[r][i >> 2][i & 3]);
+                    part += w;
+                    p[r][i >> 3][i & 7] = (_Float16)w;
+                }
+                sum[r] = fmaf(part, back, sum[r]);
+            }
+            const q8_u4* v = lds + buf * 2048 + 1024 + lane;
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const q8_half8 w = __builtin_bit_cast(q8_half8, v[64 * (2 * c + e)]);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) o[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w, p[r][e], o[r][c], 0, 0, 0);
+                }
+        }
+        __syncthreads();
+    }
+
+    // ---- lane (col, g) holds channels 16 c + 4 g + e of row col, in units of the largest scale
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        sum[r] += __shfl_xor(sum[r], 16);
+        sum[r] += __shfl_xor(sum[r], 32);
+        const int row = row0 + 16 * r + col;
+        if (row >= rows) continue;
+        const int j = row / qper;
+        const size_t to = ((size_t)n * a.m + j) * a.n_q_heads + h * qper + (row - j * qper);
+        if (a.n_split == 1) {
+            const float by = sum[r] > 0.f ? largest / sum[r] : 0.f;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+                half4 y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = (_Float16)(o[r][c][e] * by);
+                *reinterpret_cast<half4*>(a.out + to * kQ8Head + 16 * c + 4 * g) = y;
+            }
+        } else {
+            float* dst = a.partials + (to * a.n_split + split) * kQ8Partial;
+            if (g == 0) {
+                dst[0] = ref[r];
+                dst[1] = sum[r];
+            }
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dst[kPartialHeader + 16 * c + 4 * g + e] = o[r][c][e] * largest;
+        }
+    }
+}
+
+template <int KIND>
+cq_status launch(const Q8AttentionArgs& a, hipStream_t stream)
+{
+    constexpr int RB = kQ8ChunkRows / (16 * kWaves);
+    constexpr unsigned smem = 2 * 2 * 16 * 64 * 16;
+    static LdsKernelSetup setup;
+    if (setup.ensure(reinterpret_cast<const void*>(chunk_q8_kernel<KIND, RB>)) != hipSuccess) return CQ_ERR_HIP;
+    const int rows = a.m * (a.n_q_heads / a.n_kv_heads), row_blocks = (rows + kQ8ChunkRows - 1) / kQ8ChunkRows;
+    const int64_t units = (int64_t)a.batch * a.n_kv_heads * a.n_split, grid = (units + 7) / 8 * 8 * row_blocks;
+    if (grid > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
+    hipLaunchKernelGGL((chunk_q8_kernel<KIND, RB>), dim3((unsigned)grid), dim3(kThreads), smem, stream, a, row_blocks, (unsigned)units);
+    return hipGetLastError() == hipSuccess ? CQ_OK : CQ_ERR_HIP;
+}
+
+}  // namespace
+
+cq_status launch_chunk_q8(const Q8AttentionArgs& a, int kind, hipStream_t stream)
+{
+    return kind == CQ_Q8_INT8 ? launch<CQ_Q8_INT8>(a, stream) : launch<CQ_Q8_E4M3>(a, stream);
+}
+
+}  // namespace cq
