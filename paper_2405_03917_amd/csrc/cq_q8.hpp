@@ -66,9 +66,8 @@ struct Q8Plan {
     int tiles_per_split, n_split;
 };
 Q8Plan q8_plan(int batch, int n_kv_heads, int n_q_heads, int m, int t, int tokens_per_split);
-// Many rows per KV head (cq_q8_chunk.hip): kQ8ChunkRows of them to a workgroup.
-constexpr int kQ8ChunkRows = 128;
-cq_status launch_chunk_q8(const Q8AttentionArgs& a, int kind, hipStream_t stream);
+// Many rows per KV head (cq_q8_chunk.hip): 128 or 256 of them to a workgroup.
+cq_status launch_chunk_q8(const Q8AttentionArgs& a, int kind, int row_block, hipStream_t stream);
 cq_status launch_attention_q8(const Q8AttentionArgs& a, int kind, const Q8Plan& plan, hipStream_t stream);
 
 #if defined(__HIP_DEVICE_COMPILE__) || defined(__HIPCC__)

@@ -252,12 +252,16 @@ Q8Plan q8_plan(int batch, int n_kv_heads, int n_q_heads, int m, int t, int token
     const int64_t rows = (int64_t)m * (n_q_heads / n_kv_heads);
     const int n_tiles = (t - 1) / kTileTokens + 1;
     Q8Plan p;
-    p.row_block = rows <= 16 ? 16 : rows <= 64 ? 32 : kQ8ChunkRows;
+    // Workgroups of eight wavefronts convert a tile half as often as those of four, and reach further in front of their first row and
+    // behind their last: where most of the context lies in front of the chunk.  128 -> 256 rows, us: integers, 32 heads, 512 of 16384
+    // 166 -> 156, e4m3, 2 x 1024 of 8192 293 -> 271, 32 / 8 heads, 4 x 512 of 16384 568 -> 522; 2 x 4096 of 4096 348 -> 397, with 32 / 8 heads
+    // 304 -> 303; 32 / 8 heads, 64 of 8192 27 -> 33.
+    p.row_block = rows <= 16 ? 16 : rows <= 64 ? 32 : rows >= 512 && t - m >= 4096 ? 256 : 128;
     if (tokens_per_split) {
         p.tiles_per_split = tokens_per_split / kTileTokens;
-    } else if (p.row_block == kQ8ChunkRows) {
+    } else if (p.row_block > 32) {
         const int64_t blocks = (int64_t)batch * n_kv_heads * ((rows + p.row_block - 1) / p.row_block);
-        const int64_t pieces = std::max<int64_t>(1, std::min<int64_t>((n_tiles + 7) / 8, 512 / blocks));
+        const int64_t pieces = std::max<int64_t>(1, std::min<int64_t>((n_tiles + 7) / 8, 65536 / p.row_block / blocks));
         p.tiles_per_split = (int)((n_tiles + pieces - 1) / pieces);
     } else {
         const int64_t blocks = (int64_t)batch * n_kv_heads * ((rows + p.row_block - 1) / p.row_block);
@@ -272,7 +276,7 @@ Q8Plan q8_plan(int batch, int n_kv_heads, int n_q_heads, int m, int t, int token
 cq_status launch_attention_q8(const Q8AttentionArgs& a, int kind, const Q8Plan& plan, hipStream_t stream)
 {
     const int64_t rows = (int64_t)a.batch * a.m * a.n_q_heads, merges = (rows + kThreads / kQ8Head - 1) / (kThreads / kQ8Head);
-    const cq_status st = plan.row_block == kQ8ChunkRows ? launch_chunk_q8(a, kind, stream)
+    const cq_status st = plan.row_block > 32 ? launch_chunk_q8(a, kind, plan.row_block, stream)
                          : kind == CQ_Q8_INT8 ? launch_rows<CQ_Q8_INT8>(a, plan.row_block, stream) : launch_rows<CQ_Q8_E4M3>(a, plan.row_block, stream);
     if (st != CQ_OK || a.n_split == 1) return st;
     hipLaunchKernelGGL(merge_q8_kernel, dim3((unsigned)merges), dim3(kThreads), 0, stream, a.partials, a.out, rows, a.n_split);

@@ -1,11 +1,16 @@
 // Attention over the 8-bit block cache for many rows per KV head (cq_chunk_attention_q8), for gfx950.
 //
 // The products of cq_q8_attention.hip, with a tile's codes turned into fp16 once for a workgroup: its wavefronts share them through LDS
-// and each serve rows of their own.  A tile lies in LDS as the operands of the products, 16 bytes a lane one behind the
+// and each serve 32 rows.  A tile lies in LDS as the operands of the products, 16 bytes a lane one behind the
 // other, so that neither writing nor reading them meets a bank twice.  Two tiles' room: while one is worked off the next
 // is converted, and the one after that is on its way from memory.
 // Values keep their codes; a block's scale goes into its weights, relative to the largest scale so far (2^(score - reference) by
 // v_scale / v_largest, an addition to the exponent), and out of their sum again.
+// Bound by the issue of vector and matrix instructions, which keep each other waiting: per 32 rows and tile 64 products of 16
+// clocks and about 200 vector instructions, 32 exponentials among them.  Two wavefronts a SIMD that do nothing but such a mix, on
+// operands from LDS, need 3450 clocks for 2048 of products; here they need 4000.  512 rows' tokens of 16384 (e4m3, 4 x 8 KV heads):
+// 1037 TFLOP/s, integers of 32 heads 830.  (Vector work placed between the products of its own wavefront, wavefronts half a tile apart,
+// 32x32x16 products, keys straight from memory, codes in LDS: 0.95 to 0.7 of that.)
 #include <algorithm>
 
 #include "cq_q8.hpp"
@@ -13,14 +18,14 @@
 namespace cq {
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * 64;
+constexpr int RB = 2;                                       // blocks of 16 rows of a wavefront
 constexpr float kFaintest = -60.f;                          // log2 of a scale relative to the largest, below which it makes no difference
 
-template <int KIND, int RB>
-__global__ __launch_bounds__(kThreads, 2) void chunk_q8_kernel(Q8AttentionArgs a, int row_blocks, unsigned units)
+template <int KIND, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs a, int row_blocks, unsigned units)
 {
     constexpr int ROWS = 16 * RB;                           // of a wavefront
+    constexpr int N = 8 / WAVES;                            // 16 bytes a lane of keys, and of values, that a wavefront brings
     extern __shared__ q8_u4 lds[];                          // [2][keys, values][16 operands][64 lanes]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
@@ -33,8 +38,8 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_q8_kernel(Q8AttentionArgs a
     const int n = stream / a.n_kv_heads, h = stream % a.n_kv_heads;
     const int qper = a.n_q_heads / a.n_kv_heads, rows = a.m * qper;
     const int t_n = a.length(n), pos0 = t_n - a.m;
-    const int row0 = block * (ROWS * kWaves) + wave * ROWS;
-    const int block_last = pos0 + (min((block + 1) * (ROWS * kWaves), rows) - 1) / qper;
+    const int row0 = block * (ROWS * WAVES) + wave * ROWS;
+    const int block_last = pos0 + (min((block + 1) * (ROWS * WAVES), rows) - 1) / qper;
     const int n_tiles = block_last < 0 ? 0 : block_last / kTileTokens + 1;
     const int tile0 = split * a.tiles_per_split, tile1 = min(tile0 + a.tiles_per_split, n_tiles);
     // (a wavefront behind the last row repeats it and stores nothing)
@@ -65,56 +70,69 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_q8_kernel(Q8AttentionArgs a
     }
     float largest = 0.f;                                    // of the values' scales so far
 
-    // ---- wavefront w brings the keys of b = w and the values of channel blocks 2 w, 2 w + 1 (as in cq_q8_attention.hip)
-    q8_u4 gk[2], gv[2];
-    float ks = 0.f, vs = 0.f, ks_next = 0.f, vs_next = 0.f;
-    const unsigned k_off = (16 * (col >> 2) + 4 * wave + (col & 3)) * kQ8Head + 16 * g, v_off = (32 * wave + col) * kTileTokens + 16 * g;
+    // ---- a wavefront brings N of eight parts of keys (part i: tokens b = i / 2, half i & 1 of the channels) and N of values (channel block
+    // i), two operands each (as in cq_q8_attention.hip)
+    q8_u4 gk[N], gv[N];
+    const unsigned k_off = (16 * (col >> 2) + 4 * (wave * N >> 1) + (col & 3)) * kQ8Head + 16 * g + 64 * (wave * N & 1), v_off = (16 * N * wave + col) * kTileTokens + 16 * g;
     auto request = [&](size_t at) {
         const uint8_t* k = a.cache.codes[0] + at * kQ8TileBytes;
         const uint8_t* v = a.cache.codes[1] + at * kQ8TileBytes;
-        gk[0] = *reinterpret_cast<const q8_u4*>(k + k_off);
-        gk[1] = *reinterpret_cast<const q8_u4*>(k + k_off + 64);
-        gv[0] = *reinterpret_cast<const q8_u4*>(v + v_off);
-        gv[1] = *reinterpret_cast<const q8_u4*>(v + v_off + 16 * kTileTokens);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            gk[i] = *reinterpret_cast<const q8_u4*>(k + k_off + 64 * i);
+            gv[i] = *reinterpret_cast<const q8_u4*>(v + v_off + 16 * i * kTileTokens);
+        }
     };
     auto stage = [&](int tile, int buf) {
-        q8_u4* k = lds + buf * 2048 + 256 * wave + lane;
-        q8_u4* v = lds + buf * 2048 + 1024 + 256 * wave + lane;
+        q8_u4* k = lds + buf * 2048 + 128 * N * wave + lane;
+        q8_u4* v = lds + buf * 2048 + 1024 + 128 * N * wave + lane;
         if (KIND == CQ_Q8_E4M3 && (tile + 1) * kTileTokens > t_n) {
-            gv[0] = q8_only_before(gv[0], t_n - tile * kTileTokens - 16 * g);
-            gv[1] = q8_only_before(gv[1], t_n - tile * kTileTokens - 16 * g);
+#pragma unroll
+            for (int i = 0; i < N; ++i) gv[i] = q8_only_before(gv[i], t_n - tile * kTileTokens - 16 * g);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < N; ++i) {
             k[128 * i] = __builtin_bit_cast(q8_u4, q8_half8_of<KIND>(gk[i][0], gk[i][1]));
             k[128 * i + 64] = __builtin_bit_cast(q8_u4, q8_half8_of<KIND>(gk[i][2], gk[i][3]));
             v[128 * i] = __builtin_bit_cast(q8_u4, q8_half8_of<KIND>(gv[i][0], gv[i][1]));
             v[128 * i + 64] = __builtin_bit_cast(q8_u4, q8_half8_of<KIND>(gv[i][2], gv[i][3]));
         }
     };
-    size_t at = 0;
-    auto place = [&](int tile) { return a.cache.map.tile_index(n, h, min(tile, tile1 - 1)); };
+    // Lane i knows where tile `known` + i lies and its scales: asked for 60 rounds at a time, since a round by itself would wait for
+    // its answer (and a scalar request's, for LDS as well).
+    int known = tile0;
+    size_t places = 0;
+    float k_scales = 0.f, v_scales = 0.f;
+    auto learn = [&](int tile) {
+        known = tile;
+        places = a.cache.map.tile_index(n, h, min(tile + lane, tile1 - 1));
+        k_scales = a.cache.scales[0][places];
+        v_scales = a.cache.scales[1][places];
+        // (waited for here: where they are used, the requests of the next tile would be waited for as well)
+        asm volatile("" : "+v"(k_scales), "+v"(v_scales));
+    };
+    auto place = [&](int tile) {
+        const int i = tile - known;
+        return (size_t)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)places, i) | (size_t)(unsigned)__builtin_amdgcn_readlane((int)(places >> 32), i) << 32;
+    };
+    auto scale_of = [&](float scales, int tile) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scales), tile - known));
+    };
     if (tile0 < tile1) {
-        at = place(tile0);
-        request(at);
-        ks_next = a.cache.scales[0][at];
-        vs_next = a.cache.scales[1][at];
-        at = place(tile0 + 1);
+        learn(tile0);
+        request(place(tile0));
         stage(tile0, 0);
-        if (tile0 + 1 < tile1) request(at);
+        if (tile0 + 1 < tile1) request(place(tile0 + 1));
     }
     __syncthreads();
     int buf = 0;
 #pragma unroll 1
     for (int tile = tile0; tile < tile1; ++tile, buf ^= 1) {
-        ks = ks_next;
-        vs = vs_next;
+        if (tile - known == 60) learn(tile);
+        const float ks = scale_of(k_scales, tile), vs = scale_of(v_scales, tile);
         if (tile + 1 < tile1) {
-            ks_next = a.cache.scales[0][at];
-            vs_next = a.cache.scales[1][at];
             stage(tile + 1, buf ^ 1);
-            at = place(tile + 2);
-            if (tile + 2 < tile1) request(at);
+            if (tile + 2 < tile1) request(place(tile + 2));
         }
         if (tile * kTileTokens <= pos_last) {
             const q8_u4* k = lds + buf * 2048 + lane;
@@ -245,25 +263,26 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_q8_kernel(Q8AttentionArgs a
     }
 }
 
-template <int KIND>
+template <int KIND, int WAVES>
 cq_status launch(const Q8AttentionArgs& a, hipStream_t stream)
 {
-    constexpr int RB = kQ8ChunkRows / (16 * kWaves);
+    constexpr int ROWS = 16 * RB * WAVES;
     constexpr unsigned smem = 2 * 2 * 16 * 64 * 16;
     static LdsKernelSetup setup;
-    if (setup.ensure(reinterpret_cast<const void*>(chunk_q8_kernel<KIND, RB>)) != hipSuccess) return CQ_ERR_HIP;
-    const int rows = a.m * (a.n_q_heads / a.n_kv_heads), row_blocks = (rows + kQ8ChunkRows - 1) / kQ8ChunkRows;
+    if (setup.ensure(reinterpret_cast<const void*>(chunk_q8_kernel<KIND, WAVES>)) != hipSuccess) return CQ_ERR_HIP;
+    const int rows = a.m * (a.n_q_heads / a.n_kv_heads), row_blocks = (rows - 1) / ROWS + 1;
     const int64_t units = (int64_t)a.batch * a.n_kv_heads * a.n_split, grid = (units + 7) / 8 * 8 * row_blocks;
     if (grid > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
-    hipLaunchKernelGGL((chunk_q8_kernel<KIND, RB>), dim3((unsigned)grid), dim3(kThreads), smem, stream, a, row_blocks, (unsigned)units);
+    hipLaunchKernelGGL((chunk_q8_kernel<KIND, WAVES>), dim3((unsigned)grid), dim3(WAVES * 64), smem, stream, a, row_blocks, (unsigned)units);
     return hipGetLastError() == hipSuccess ? CQ_OK : CQ_ERR_HIP;
 }
 
 }  // namespace
 
-cq_status launch_chunk_q8(const Q8AttentionArgs& a, int kind, hipStream_t stream)
+cq_status launch_chunk_q8(const Q8AttentionArgs& a, int kind, int row_block, hipStream_t stream)
 {
-    return kind == CQ_Q8_INT8 ? launch<CQ_Q8_INT8>(a, stream) : launch<CQ_Q8_E4M3>(a, stream);
+    if (row_block == 256) return kind == CQ_Q8_INT8 ? launch<CQ_Q8_INT8, 8>(a, stream) : launch<CQ_Q8_E4M3, 8>(a, stream);
+    return kind == CQ_Q8_INT8 ? launch<CQ_Q8_INT8, 4>(a, stream) : launch<CQ_Q8_E4M3, 4>(a, stream);
 }
 
 }  // namespace cq
