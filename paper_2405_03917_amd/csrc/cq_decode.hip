@@ -345,6 +345,12 @@ cq_status launch_format(const Args& a, hipStream_t stream)
 
 }  // namespace
 
+unsigned* merge_counters_for(hipStream_t stream, int rows)
+{
+    // (that handle is another stream in every thread)
+    return stream == hipStreamPerThread ? nullptr : g_merge_counters.for_stream(stream, rows);
+}
+
 cq_status launch_layer_table_write(const LayerChunk& chunk, int count, LayerPtrs* dst, hipStream_t stream)
 {
     hipLaunchKernelGGL(layer_table_write_kernel, dim3(1), dim3(64), 0, stream, chunk, count, dst);

@@ -304,6 +304,8 @@ cq_status launch_kmeans(const KMeansArgs& a, void* workspace, hipStream_t stream
 cq_status launch_encode(const EncodeArgs& a, hipStream_t stream);
 // many tokens per sequence: the MFMA-filtered kernel (cq_encode_mfma.hip)
 cq_status launch_encode_tiles(const EncodeArgs& a, hipStream_t stream);
+// arrival counters of a launch's rows for an in-kernel merge (null: the stream has none, a merge kernel has to follow)
+unsigned* merge_counters_for(hipStream_t stream, int rows);
 cq_status launch_decode(const DecodeArgs& a, hipStream_t stream);
 cq_status launch_decode_view(const DecodeViewArgs& a, hipStream_t stream);
 // cq_decode_weights.hip: behind an attention kernel that wrote scores and partials, the accumulators, and (several splits)

@@ -8,6 +8,7 @@ namespace cq {
 constexpr int kQ8Head = 128;                                // channels of a head
 constexpr int kQ8TileBytes = kTileTokens * kQ8Head;         // of keys [token][channel] or of values [channel][token]
 constexpr int kQ8Pairs = kQ8Head / 2;
+constexpr int kQ8RowTiles = 256;                           // most tiles of a piece of the context where a KV head has few rows
 constexpr int kQ8Partial = kQ8Head + kPartialHeader;        // floats of a partial row: reference, sum, channels
 
 struct Q8Cache {
@@ -59,6 +60,17 @@ struct Q8AttentionArgs : Q8Rows {
     int n_q_heads;
     int tiles_per_split, n_split;
     float* partials;                                        // [batch][m][n_q_heads][n_split][kQ8Partial]
+    int row_block;                                          // rows of a KV head that a workgroup serves
+    unsigned* counters;                                     // arrivals per (stream, row block); null: merge_q8_kernel follows
+
+    // Tiles that the rows of a block look at, and how many pieces of the context have any (one at least: it writes the rows of
+    // sequences of no tokens).  A row block of one piece goes to the output at once.
+    __device__ __forceinline__ int block_tiles(int t_n, int block) const
+    {
+        const int qper = n_q_heads / n_kv_heads, last = (min((block + 1) * row_block, m * qper) - 1) / qper;
+        return max((t_n - m + last + kTileTokens) / kTileTokens, 0);
+    }
+    __device__ __forceinline__ int pieces(int n_tiles) const { return max((n_tiles - 1) / tiles_per_split + 1, 1); }
 };
 // How a call is cut: which kernel, tiles per split.  A function of the sizes alone.
 struct Q8Plan {

@@ -7,7 +7,9 @@
 // KV head (query heads of a token, tokens of a chunk) in the 16 columns.  The result of S^T holds, in the lane of column n
 // and block g, rows 4 g + e; rows of key tile b are tokens 16 g + 4 b + e, so a lane's scores of b = 0 .. 3 are tokens 16 g .. 16 g + 15, in
 // order: what the lane feeds into the second product, whose other operand (16 tokens of a channel) is 16 bytes of the cache as they lie.
-// Bound by memory: 16 KB a tile against 512 products' clocks and about 1000 of conversions.
+// Bound by memory: 16 KB a tile against 512 products' clocks and about 1000 of conversions.  16 x 32 streams of 8192 tokens, 1.07 GB: 178 us,
+// 6.0 TB/s of the 6.4 that a large copy reads at; 24 x 8 of 6007 at most, paged e4m3, 167 MB: 43 us, 3.9; 8 of 2000, 4 MB: 9.0 us, most of it the
+// way of a first request and of the merge.
 #include <algorithm>
 
 #include "cq_q8.hpp"
@@ -17,49 +19,113 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
-// One row's weighted values from its pieces: `n` of (reference, sum, 128 channels), `stride` floats apart; channel i.
-__device__ __forceinline__ float merged(const float* p, int n, size_t stride, int i)
+// Partial rows go from workgroup to workgroup two floats at a time; within a running kernel by device-scope accesses, written through
+// to where every workgroup's loads find them.
+typedef float float2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void put2(float* p, float x, float y, bool within)
 {
-    float m = kQ8Lowest, l = 0.f, o = 0.f;
-#pragma unroll 4
-    for (int s = 0; s < n; ++s) {
-        const float ms = p[s * stride], ls = p[s * stride + 1], os = p[s * stride + kPartialHeader + i];
-        const float m_new = fmaxf(m, ms);
-        const float keep = __builtin_amdgcn_exp2f(m - m_new), w = __builtin_amdgcn_exp2f(ms - m_new);
-        // (a piece without tokens leaves its channels unwritten)
-        l = fmaf(l, keep, ls * w);
-        o = fmaf(o, keep, ls > 0.f ? os * w : 0.f);
-        m = m_new;
-    }
-    return l > 0.f ? o / l : 0.f;
+    if (!within) *reinterpret_cast<float2_t*>(p) = float2_t{x, y};
+    else __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), __builtin_bit_cast(unsigned long long, float2_t{x, y}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <bool WITHIN>
+__device__ __forceinline__ float2_t get2(const float* p)
+{
+    if (!WITHIN) return *reinterpret_cast<const float2_t*>(p);
+    return __builtin_bit_cast(float2_t, __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 
-__global__ __launch_bounds__(kThreads) void merge_q8_kernel(const float* partials, uint16_t* out, int64_t rows, int n_split)
+// Rows row0 .. row0 + count - 1 (32 at most) of a stream from their `pieces` partials (reference, sum, 128 channels), by a workgroup: 16
+// lanes take 8 channels each of a row, or, of few rows, of every second, fourth, ... of its pieces.  One pass with a running
+// reference, requests of four pieces together; then those of a row meet in LDS, and are rounded to fp16 once.
+struct MergeLds {
+    float part[16][16][10];                                 // [group][lane]: reference, sum, channels
+};
+template <bool WITHIN>
+__device__ __forceinline__ void merge_rows(const Q8AttentionArgs& a, int n, int h, int row0, int count, int pieces, MergeLds& lds, int tid)
 {
-    const int64_t row = (int64_t)blockIdx.x * (kThreads / kQ8Head) + threadIdx.x / kQ8Head;
-    const int i = threadIdx.x % kQ8Head;
-    if (row >= rows) return;
-    const _Float16 h = (_Float16)merged(partials + row * n_split * kQ8Partial, n_split, kQ8Partial, i);
-    out[row * kQ8Head + i] = __builtin_bit_cast(uint16_t, h);
+    const int qper = a.n_q_heads / a.n_kv_heads, group = tid >> 4, lane = tid & 15;
+    const int share = count <= 1 ? 16 : count <= 2 ? 8 : count <= 4 ? 4 : count <= 8 ? 2 : 1;
+    const int first = group / share, at_once = 16 / share;  // rows first, first + at_once, ...
+    for (int base = 0; base < count; base += at_once) {
+        const int row = row0 + base + first, j = row / qper;
+        const bool mine = base + first < count;
+        const size_t at = ((size_t)n * a.m + j) * a.n_q_heads + h * qper + (row - j * qper);
+        float m = kQ8Lowest, l = 0.f, y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = 0.f;
+        if (mine) {
+            const float* p = a.partials + (at * a.n_split + group % share) * kQ8Partial;
+#pragma unroll 4
+            for (int s = group % share; s < pieces; s += share, p += share * kQ8Partial) {
+                const float2_t head = get2<WITHIN>(p);
+                float2_t x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = get2<WITHIN>(p + kPartialHeader + 8 * lane + 2 * e);
+                const float now = fmaxf(m, head[0]), keep = __builtin_amdgcn_exp2f(m - now), w = __builtin_amdgcn_exp2f(head[0] - now);
+                l = fmaf(l, keep, head[1] * w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = fmaf(y[e], keep, x[e >> 1][e & 1] * w);
+                m = now;
+            }
+        }
+        if (share > 1) {
+            __syncthreads();
+            float* mine_at = lds.part[group][lane];
+            mine_at[0] = m;
+            mine_at[1] = l;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) mine_at[2 + e] = y[e];
+            __syncthreads();
+            if (group % share == 0) {
+                for (int s = 1; s < share; ++s) {
+                    const float* x = lds.part[group + s][lane];
+                    const float now = fmaxf(m, x[0]), keep = __builtin_amdgcn_exp2f(m - now), w = __builtin_amdgcn_exp2f(x[0] - now);
+                    l = fmaf(l, keep, x[1] * w);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = fmaf(y[e], keep, x[2 + e] * w);
+                    m = now;
+                }
+            }
+        }
+        if (mine && group % share == 0) {
+            q8_half8 z;
+            const float by = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = (_Float16)(y[e] * by);
+            *reinterpret_cast<q8_half8*>(a.out + at * kQ8Head + 8 * lane) = z;
+        }
+    }
+}
+
+// A workgroup per 32 rows (16, where a workgroup of the kernel in front served as many).
+__global__ __launch_bounds__(kThreads) void merge_q8_kernel(Q8AttentionArgs a, int blocks, int block_rows)
+{
+    __shared__ MergeLds lds;
+    const int block = blockIdx.x % blocks, stream = blockIdx.x / blocks;
+    const int n = stream / a.n_kv_heads, h = stream % a.n_kv_heads, row0 = block * block_rows;
+    const int pieces = a.pieces(a.block_tiles(a.length(n), row0 / a.row_block));
+    if (pieces > 1) merge_rows<false>(a, n, h, row0, min(block_rows, a.m * (a.n_q_heads / a.n_kv_heads) - row0), pieces, lds, threadIdx.x);
 }
 
 template <int KIND, int RB>
-__global__ __launch_bounds__(kThreads) void rows_q8_kernel(Q8AttentionArgs a, int row_blocks, unsigned units)
+__global__ __launch_bounds__(kThreads, 2) void rows_q8_kernel(Q8AttentionArgs a, int row_blocks, unsigned units)
 {
     __shared__ float lds[kWaves][16 * RB][kQ8Partial];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
-    // the row blocks of a piece of a stream run on one XCD, which shares what it reads
+    // the row blocks of a piece of a stream run on one XCD, which shares what it reads; all streams' first pieces are dealt out, then all
+    // second ones: the heads of a sequence have the same pieces to do, and the XCDs as many of them each
     const unsigned eighth = blockIdx.x >> 3;
     const int block = eighth % row_blocks;
     const unsigned unit = (eighth / row_blocks) * 8 + (blockIdx.x & 7);
     if (unit >= units) return;
-    const int split = unit % a.n_split, stream = unit / a.n_split;
+    const unsigned streams = (unsigned)(a.batch * a.n_kv_heads);
+    const int split = unit / streams, stream = unit % streams;
     const int n = stream / a.n_kv_heads, h = stream % a.n_kv_heads;
     const int qper = a.n_q_heads / a.n_kv_heads, rows = a.m * qper, row0 = block * 16 * RB;
-    const int t_n = a.length(n), pos0 = t_n - a.m;
-    const int pos_first = pos0 + row0 / qper, pos_last = pos0 + (min(row0 + 16 * RB, rows) - 1) / qper;
-    const int n_tiles = pos_last < 0 ? 0 : pos_last / kTileTokens + 1;
+    const int t_n = a.length(n), pos0 = t_n - a.m, pos_first = pos0 + row0 / qper;
+    const int n_tiles = a.block_tiles(t_n, block), pieces = a.pieces(n_tiles);
+    if (split >= pieces) return;
     const int tile0 = split * a.tiles_per_split, tile1 = min(tile0 + a.tiles_per_split, n_tiles);
     const float scale = fabsf(a.scale_log2e);
 
@@ -86,30 +152,37 @@ __global__ __launch_bounds__(kThreads) void rows_q8_kernel(Q8AttentionArgs a, in
         for (int c = 0; c < 8; ++c) o[r][c] = q8_float4{0.f, 0.f, 0.f, 0.f};
     }
 
+    // Codes of a tile: the next one's keys and values each take the place of those they follow.  (Two tiles' registers, all of the next requested
+    // ahead of this one's work, are 2 wavefronts a SIMD instead of 3 for integers: 8 heads x 65536 tokens 28 -> 30 us.)
     q8_u4 kr[8], vr[8];
-    float ks = 0.f, vs = 0.f;
     auto request_keys = [&](size_t at) {
         const uint8_t* src = a.cache.codes[0] + at * kQ8TileBytes + (16 * (col >> 2) + (col & 3)) * kQ8Head + 16 * g;
 #pragma unroll
         for (int i = 0; i < 8; ++i) kr[i] = *reinterpret_cast<const q8_u4*>(src + 4 * (i >> 1) * kQ8Head + 64 * (i & 1));
-        ks = a.cache.scales[0][at];
     };
     auto request_values = [&](size_t at) {
         const uint8_t* src = a.cache.codes[1] + at * kQ8TileBytes + col * kTileTokens + 16 * g;
 #pragma unroll
         for (int i = 0; i < 8; ++i) vr[i] = *reinterpret_cast<const q8_u4*>(src + 16 * i * kTileTokens);
-        vs = a.cache.scales[1][at];
     };
-    int tile = tile0 + wave;
-    if (tile < tile1) {
-        const size_t at = a.cache.map.tile_index(n, h, tile);
-        request_keys(at);
-        request_values(at);
+    // lane i knows where the i-th of this wavefront's tiles (64 at most: kQ8RowTiles) lies, and its scales: none is asked for by itself
+    // (those behind the sequence's end lie somewhere in the pool, unused; its length is not waited for)
+    const int count = max(tile1 - tile0 - wave + kWaves - 1, 0) / kWaves;
+    const size_t places = a.cache.map.tile_index(n, h, min(tile0 + wave + kWaves * lane, (a.t - 1) / kTileTokens));
+    const float k_scales = a.cache.scales[0][places], v_scales = a.cache.scales[1][places];
+    auto place = [&](int i) {
+        return (size_t)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)places, i) | (size_t)(unsigned)__builtin_amdgcn_readlane((int)(places >> 32), i) << 32;
+    };
+    auto scale_of = [&](float scales, int i) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scales), i)); };
+    if (count > 0) {
+        request_keys(place(0));
+        request_values(place(0));
     }
 #pragma unroll 1
-    for (; tile < tile1; tile += kWaves) {
-        const bool more = tile + kWaves < tile1;
-        const size_t next = a.cache.map.tile_index(n, h, more ? tile + kWaves : tile);
+    for (int t = 0; t < count; ++t) {
+        const int tile = tile0 + wave + kWaves * t;
+        const bool more = t + 1 < count;
+        const size_t next = place(more ? t + 1 : t);
         q8_float4 s[RB][4];
 #pragma unroll
         for (int r = 0; r < RB; ++r)
@@ -128,7 +201,7 @@ __global__ __launch_bounds__(kThreads) void rows_q8_kernel(Q8AttentionArgs a, in
                 }
             }
         // (a factor of zero stands for one so small that every weight is 1: 0 times a masked -infinity is no number)
-        const float by = fmaxf(scale * ks, 1e-37f);
+        const float by = fmaxf(scale * scale_of(k_scales, t), 1e-37f);
         if (more) request_keys(next);
         const int first = tile * kTileTokens + 16 * g;
         q8_half8 p[RB][2];
@@ -165,11 +238,13 @@ __global__ __launch_bounds__(kThreads) void rows_q8_kernel(Q8AttentionArgs a, in
 #pragma unroll
             for (int i = 0; i < 16; ++i) p[r][i >> 3][i & 7] = (_Float16)w[i];
         }
-        const bool cut = KIND == CQ_Q8_E4M3 && (tile + 1) * kTileTokens > t_n;
+        const float vs = scale_of(v_scales, t);
+        // e4m3 bytes of tokens that are not there may be no numbers, and a weight of zero would not hide them
+        q8_u4 there = {~0u, ~0u, ~0u, ~0u};
+        if (KIND == CQ_Q8_E4M3 && (tile + 1) * kTileTokens > t_n) there = q8_only_before(there, t_n - first);
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
-            q8_u4 w = vr[c];
-            if (cut) w = q8_only_before(w, t_n - first);
+            const q8_u4 w = KIND == CQ_Q8_E4M3 ? vr[c] & there : vr[c];
             const q8_half8 v0 = q8_half8_of<KIND>(w[0], w[1]), v1 = q8_half8_of<KIND>(w[2], w[3]);
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
@@ -217,21 +292,36 @@ __global__ __launch_bounds__(kThreads) void rows_q8_kernel(Q8AttentionArgs a, in
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = fmaf(lds[w][local][kPartialHeader + i0 + i], by, y[i]);
         }
-        if (a.n_split == 1) {
+        if (pieces == 1) {
             q8_half8 z;
+            const float by = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = (_Float16)(l > 0.f ? y[i] / l : 0.f);
+            for (int i = 0; i < 8; ++i) z[i] = (_Float16)(y[i] * by);
             *reinterpret_cast<q8_half8*>(a.out + at * kQ8Head + i0) = z;
         } else {
             float* dst = a.partials + (at * a.n_split + split) * kQ8Partial;
-            if ((tid & 15) == 0) {
-                dst[0] = m;
-                dst[1] = l;
-            }
+            if ((tid & 15) == 0) put2(dst, m, l, a.counters);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dst[kPartialHeader + i0 + i] = y[i];
+            for (int i = 0; i < 8; i += 2) put2(dst + kPartialHeader + i0 + i, y[i], y[i + 1], a.counters);
         }
     }
+    if (pieces == 1 || !a.counters) return;
+    // ---- the last piece to finish merges them all: every wavefront waits for its stores (a barrier does not), all meet, one
+    // thread counts the workgroup in, and the last of them takes the counter back to zero for the next call
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    unsigned* flag = reinterpret_cast<unsigned*>(&lds[0][0][0]);
+    if (tid == 0) {
+        unsigned* counter = a.counters + (size_t)stream * row_blocks + block;
+        const bool last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)pieces - 1u;
+        if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *flag = last;
+    }
+    __syncthreads();
+    if (*flag == 0u) return;
+    static_assert(sizeof(MergeLds) <= sizeof(lds), "the merge takes the rows' place");
+    __syncthreads();                                        // (the flag is read)
+    merge_rows<true>(a, n, h, row0, min(16 * RB, rows - row0), pieces, *reinterpret_cast<MergeLds*>(&lds[0][0][0]), tid);
 }
 
 template <int KIND>
@@ -258,28 +348,42 @@ Q8Plan q8_plan(int batch, int n_kv_heads, int n_q_heads, int m, int t, int token
     // 304 -> 303; 32 / 8 heads, 64 of 8192 27 -> 33.
     p.row_block = rows <= 16 ? 16 : rows <= 64 ? 32 : rows >= 512 && t - m >= 4096 ? 256 : 128;
     if (tokens_per_split) {
-        p.tiles_per_split = tokens_per_split / kTileTokens;
+        p.tiles_per_split = p.row_block > 32 ? tokens_per_split / kTileTokens : std::min(tokens_per_split / kTileTokens, kQ8RowTiles);
     } else if (p.row_block > 32) {
         const int64_t blocks = (int64_t)batch * n_kv_heads * ((rows + p.row_block - 1) / p.row_block);
         const int64_t pieces = std::max<int64_t>(1, std::min<int64_t>((n_tiles + 7) / 8, 65536 / p.row_block / blocks));
         p.tiles_per_split = (int)((n_tiles + pieces - 1) / pieces);
     } else {
+        // A workgroup costs about 5 us besides its tiles (its way to the first codes, its partials), so there is one round of them: two to
+        // a CU, or one where there are few streams, whose pieces then are fewer to merge.  us by workgroups: 24 x 8 streams of 6007 at
+        // most, e4m3, 192 53, 384 45, 576 43, 1152 43, 2304 44; 8 of 65536 128 39, 256 28, 512 28, 1024 31, 2048 38; 32 of 4096 128 14, 256 12,
+        // 512 13; 512 of 8192 512 178, 1024 185, 4096 188.
         const int64_t blocks = (int64_t)batch * n_kv_heads * ((rows + p.row_block - 1) / p.row_block);
-        const int64_t pieces = std::max<int64_t>(1, std::min<int64_t>((n_tiles + kWaves - 1) / kWaves, 1024 / blocks));
+        const int64_t wanted = blocks >= 64 ? (512 + blocks / 2) / blocks : (255 + blocks) / blocks;
+        const int64_t pieces = std::max<int64_t>(1, std::min<int64_t>((n_tiles + kWaves - 1) / kWaves, wanted));
         const int64_t tiles = (n_tiles + pieces - 1) / pieces;
-        p.tiles_per_split = (int)((tiles + kWaves - 1) / kWaves * kWaves);
+        p.tiles_per_split = (int)std::min<int64_t>((tiles + kWaves - 1) / kWaves * kWaves, kQ8RowTiles);
     }
     p.n_split = (n_tiles - 1) / p.tiles_per_split + 1;
     return p;
 }
 
-cq_status launch_attention_q8(const Q8AttentionArgs& a, int kind, const Q8Plan& plan, hipStream_t stream)
+cq_status launch_attention_q8(const Q8AttentionArgs& args, int kind, const Q8Plan& plan, hipStream_t stream)
 {
-    const int64_t rows = (int64_t)a.batch * a.m * a.n_q_heads, merges = (rows + kThreads / kQ8Head - 1) / (kThreads / kQ8Head);
-    const cq_status st = plan.row_block > 32 ? launch_chunk_q8(a, kind, plan.row_block, stream)
+    Q8AttentionArgs a = args;
+    a.row_block = plan.row_block;
+    const bool chunk = plan.row_block > 32;
+    const int64_t blocks = (int64_t)a.batch * a.n_kv_heads * ((a.m * (a.n_q_heads / a.n_kv_heads) - 1) / plan.row_block + 1);
+    // Merging within the kernel saves a launch, and costs each workgroup the way of its partials to memory and back: for small calls
+    // (8 streams of 2000 tokens 10.0 -> 9.0 us, 32 of 4096 12.7 -> 12.3; 256 workgroups in 32 pieces a stream 10.4 -> 12).
+    a.counters = chunk || a.n_split == 1 || a.n_split > 8 || blocks * a.n_split > 256 ? nullptr : merge_counters_for(stream, (int)blocks);
+    const cq_status st = chunk                 ? launch_chunk_q8(a, kind, plan.row_block, stream)
                          : kind == CQ_Q8_INT8 ? launch_rows<CQ_Q8_INT8>(a, plan.row_block, stream) : launch_rows<CQ_Q8_E4M3>(a, plan.row_block, stream);
-    if (st != CQ_OK || a.n_split == 1) return st;
-    hipLaunchKernelGGL(merge_q8_kernel, dim3((unsigned)merges), dim3(kThreads), 0, stream, a.partials, a.out, rows, a.n_split);
+    if (st != CQ_OK || a.n_split == 1 || a.counters) return st;
+    const int block_rows = std::min(plan.row_block, 32), row_blocks = (a.m * (a.n_q_heads / a.n_kv_heads) - 1) / block_rows + 1;
+    const int64_t grid = (int64_t)a.batch * a.n_kv_heads * row_blocks;
+    if (grid > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
+    hipLaunchKernelGGL(merge_q8_kernel, dim3((unsigned)grid), dim3(kThreads), 0, stream, a, row_blocks, block_rows);
     return hipGetLastError() == hipSuccess ? CQ_OK : CQ_ERR_HIP;
 }
 

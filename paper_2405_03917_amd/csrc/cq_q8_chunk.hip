@@ -39,8 +39,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs
     const int qper = a.n_q_heads / a.n_kv_heads, rows = a.m * qper;
     const int t_n = a.length(n), pos0 = t_n - a.m;
     const int row0 = block * (ROWS * WAVES) + wave * ROWS;
-    const int block_last = pos0 + (min((block + 1) * (ROWS * WAVES), rows) - 1) / qper;
-    const int n_tiles = block_last < 0 ? 0 : block_last / kTileTokens + 1;
+    const int n_tiles = a.block_tiles(t_n, block), pieces = a.pieces(n_tiles);
+    if (split >= pieces) return;
     const int tile0 = split * a.tiles_per_split, tile1 = min(tile0 + a.tiles_per_split, n_tiles);
     // (a wavefront behind the last row repeats it and stores nothing)
     const int pos_first = pos0 + min(row0, rows - 1) / qper, pos_last = pos0 + (min(row0 + ROWS, rows) - 1) / qper;
@@ -239,7 +239,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs
         if (row >= rows) continue;
         const int j = row / qper;
         const size_t to = ((size_t)n * a.m + j) * a.n_q_heads + h * qper + (row - j * qper);
-        if (a.n_split == 1) {
+        if (pieces == 1) {
             const float by = sum[r] > 0.f ? largest / sum[r] : 0.f;
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
