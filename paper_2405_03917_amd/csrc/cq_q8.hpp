@@ -29,7 +29,7 @@ struct Q8AppendArgs : Q8Rows {
     int64_t x_batch_stride, x_row_stride;
     Q8Cache cache;
     const double2* tile_tab;                                // cos, sin of 64 tile theta_i: [tile][pair] (null: no rotation)
-    const double2* lane_tab;                                // cos, sin of u theta_i: [u][pair]
+    const double2* lane_tab;                                // cos, sin of u theta_i: in the order of lane_entry
     const uint16_t* q;                                      // queries to rotate (null: none), by strides
     int64_t q_batch_stride, q_row_stride;
     int n_q_heads;

@@ -7,10 +7,12 @@
 //   code = nearest(x / s), ties to even; codes of older tokens, where s grew: nearest(c s_before / s)
 //
 // Which side of a border a number lies on is decided in 64 bits (angles are products of two table entries in 64 bits): codes are
-// those of exact arithmetic but for borders met to 2^-50, whatever the position, and do not depend on how a call is cut.
-// fp64 costs what fp32 does here (no packed fp32), and the kernel is bound by memory.
+// those of exact arithmetic but for borders met to 2^-45, whatever the position, and do not depend on how a call is cut.
+// fp64 costs what fp32 does here (no packed fp32), but for conversions; of values, which are fp16, fp32 decides where it can.
 // e4m3 scales are powers of two so that a growing scale moves codes without rounding them again (but into
 // subnormals); integers use the whole range instead: a power of two would cost up to a bit of seven.
+// Bound by memory where there is much of it: 4 x 8192 tokens of 8 heads with 32 heads' queries, 738 MB, 153 us; 6 x 500 of 32 heads, 123 MB, 44 us, of
+// few workgroups with a reduction each; single tokens by latency: length, page, scale, reduction, division, one after another.
 #include <algorithm>
 
 #include "cq_q8.hpp"
@@ -20,45 +22,62 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// x rounded to fp32 so that rounding once more, to fewer bits, is right: towards zero, and the last bit set if something was cut off.
+// A number in units of its block's scale (127 or 448 at most, but for the rounding of a scale) as its code byte, with other bits
+// above it.  Integers: the sum with 1.5 x 2^52 has the nearest one in its last bits.  e4m3: x rounded to fp32 so that rounding once
+// more is right: what lies below the 20 upper bits of the mantissa becomes one bit under them; zero, of either sign, has one code.
+constexpr double kMagic64 = 6755399441055744.0;
+constexpr float kMagic32 = 12582912.f;
+__device__ __forceinline__ unsigned low_word(double x) { return (unsigned)__builtin_bit_cast(unsigned long long, x); }
 __device__ __forceinline__ float to_odd(double x)
 {
-    float f = (float)x;
-    const double back = (double)f;
-    if (back != x) {
-        unsigned b = __builtin_bit_cast(unsigned, f);
-        if (fabs(back) > fabs(x)) b -= 1;
-        f = __builtin_bit_cast(float, b | 1u);
-    }
-    return f;
+    const unsigned long long b = __builtin_bit_cast(unsigned long long, x + 0.0);
+    return (float)__builtin_bit_cast(double, (b & 0xffffffff00000000ULL) | ((unsigned)b ? 0x20000000u : 0u));
 }
-
-// The code byte of a number in units of its block's scale.
-template <int KIND>
-__device__ __forceinline__ unsigned code_of(double x)
+// Four such bytes of integers' sums, and of e4m3 numbers in fp32, as a word of the cache.
+__device__ __forceinline__ unsigned pack_integers(unsigned a, unsigned b, unsigned c, unsigned d)
 {
-    if constexpr (KIND == CQ_Q8_INT8) {
-        const int c = (int)fmin(fmax(rint(x), -127.0), 127.0);
-        return (unsigned)(c + 128);
-    } else {
-        const float f = fminf(fmaxf(to_odd(x), -448.f), 448.f) + 0.f;         // (zero, of either sign, has one code)
-        return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(f, f, 0, false) & 0xffu;
-    }
+    const unsigned lo = __builtin_amdgcn_perm(b, a, 0x0c0c0400u), hi = __builtin_amdgcn_perm(d, c, 0x04000c0cu);
+    return (lo | hi) ^ 0x80808080u;
 }
-// ... of code byte w's number under a scale that grew by 1 / ratio.
-template <int KIND>
-__device__ __forceinline__ unsigned regrown(unsigned w, double ratio)
+__device__ __forceinline__ unsigned pack_e4m3(float a, float b, float c, float d)
 {
-    if constexpr (KIND == CQ_Q8_INT8) return code_of<KIND>((double)((int)w - 128) * ratio);
-    else return code_of<KIND>((double)__builtin_amdgcn_cvt_f32_fp8((int)w, 0) * ratio);
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
+// x / s of an s whose reciprocal is `inv`, as IEEE division gives it (but for quotients no code depends on).
+__device__ __forceinline__ double quotient(double x, double s, double inv)
+{
+    const double y = x * inv;
+    return fma(fma(-y, s, x), inv, y);
+}
+// x / s, four of them.  (An e4m3 scale is a power of two.)
+template <int KIND>
+__device__ __forceinline__ unsigned codes4(const double* x, double s, double inv)
+{
+    if constexpr (KIND == CQ_Q8_INT8)
+        return pack_integers(low_word(quotient(x[0], s, inv) + kMagic64), low_word(quotient(x[1], s, inv) + kMagic64), low_word(quotient(x[2], s, inv) + kMagic64),
+                             low_word(quotient(x[3], s, inv) + kMagic64));
+    else return pack_e4m3(to_odd(x[0] * inv), to_odd(x[1] * inv), to_odd(x[2] * inv), to_odd(x[3] * inv));
+}
+// Four codes under a scale that grew by 1 / ratio.
 template <int KIND>
 __device__ __forceinline__ unsigned regrown4(unsigned w, double ratio)
 {
-    unsigned r = 0;
+    double x[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r |= regrown<KIND>((w >> (8 * i)) & 0xffu, ratio) << (8 * i);
-    return r;
+    for (int i = 0; i < 4; ++i) {
+        const unsigned byte = (w >> (8 * i)) & 0xffu;
+        x[i] = KIND == CQ_Q8_INT8 ? (double)((int)byte - 128) : (double)__builtin_amdgcn_cvt_f32_fp8((int)byte, 0);
+    }
+    if constexpr (KIND == CQ_Q8_INT8)
+        return pack_integers(low_word(fma(x[0], ratio, kMagic64)), low_word(fma(x[1], ratio, kMagic64)), low_word(fma(x[2], ratio, kMagic64)), low_word(fma(x[3], ratio, kMagic64)));
+    else return codes4<KIND>(x, 1.0, ratio);
+}
+template <int KIND>
+__device__ __forceinline__ q8_u4 regrown16(q8_u4 w, double ratio)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = regrown4<KIND>(w[i], ratio);
+    return w;
 }
 
 template <int KIND>
@@ -69,17 +88,14 @@ __device__ __forceinline__ float need_of(double largest)
     return (float)__builtin_bit_cast(double, (bits + 0xfffffffffffffULL) & (0x7ffULL << 52));
 }
 
-// x / s of an s whose reciprocal is `inv`, as IEEE division gives it (but for quotients no code depends on).
-__device__ __forceinline__ double quotient(double x, double s, double inv)
-{
-    const double y = x * inv;
-    return fma(fma(-y, s, x), inv, y);
-}
-
-__device__ __forceinline__ double wave_max_f64(double x)
+template <class T>
+__device__ __forceinline__ T wave_max(T x)
 {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) x = fmax(x, __shfl_xor(x, d));
+    for (int d = 1; d < 64; d *= 2) {
+        const T y = __shfl_xor(x, d);
+        x = x > y ? x : y;
+    }
     return x;
 }
 
@@ -89,6 +105,13 @@ __device__ __forceinline__ void halves_of(q8_u4 w, double* x)
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (double)(float)h[i];
 }
+// the larger magnitude of two pairs of fp16 numbers, as bits
+typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ unsigned larger_halves(unsigned a, unsigned b)
+{
+    return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(ushort2_t, a), __builtin_bit_cast(ushort2_t, b & 0x7fff7fffu)));
+}
+__device__ __forceinline__ float largest_half(unsigned w) { return (float)__builtin_bit_cast(_Float16, (unsigned short)max(w & 0xffffu, w >> 16)); }
 
 // cos, sin of (64 tile + u) theta_i
 __device__ __forceinline__ double2 angle_of(double2 tile, double2 lane)
@@ -96,73 +119,142 @@ __device__ __forceinline__ double2 angle_of(double2 tile, double2 lane)
     return make_double2(fma(tile.x, lane.x, -tile.y * lane.y), fma(tile.y, lane.x, tile.x * lane.y));
 }
 
-// The block's scale from the largest new magnitude of every thread; `grown`: the older tokens' codes change by `ratio`.
+// Where the entry of pair i and token u lies in the second half of the table: [i % 16][u][i / 16], so that threads of the kernel
+// that writes tiles, 16 pairs of a token each, read 1 KB of it together.
+__device__ __forceinline__ int lane_entry(int u, int i) { return ((i & 15) * kTileTokens + u) * (kQ8Pairs / 16) + (i >> 4); }
+
+// A block's scale from the largest new magnitude and the scale before (0 of a block that holds no older tokens); `grown`: the
+// older tokens' codes change by `ratio`.
 struct BlockScale {
+    float scale;
     double s, inv, ratio;
     bool grown;
 };
 template <int KIND>
-__device__ __forceinline__ BlockScale block_scale(double mine, bool has_old, float* at, double* lds, int tid)
+__device__ __forceinline__ BlockScale block_scale(double largest, bool has_old, float before)
 {
-    const double w = wave_max_f64(mine);
-    __syncthreads();                                        // (the reads of the head before are done)
-    if ((tid & 63) == 0) lds[tid >> 6] = w;
-    if (tid == 0) lds[4] = has_old ? (double)*at : 0.0;     // (the thread that writes it is the only one that reads it)
-    __syncthreads();
-    const double largest = fmax(fmax(lds[0], lds[1]), fmax(lds[2], lds[3]));
-    const float before = (float)lds[4];
-    const float s = fmaxf(before, need_of<KIND>(largest));
-    if (tid == 0) *at = s;
     BlockScale b;
-    b.s = s;
-    b.inv = s > 0.f ? 1.0 / (double)s : 0.0;
-    b.grown = has_old && s > before;
-    b.ratio = b.grown ? (double)before / (double)s : 1.0;
+    b.scale = fmaxf(before, need_of<KIND>(largest));
+    b.s = b.scale;
+    b.inv = b.scale > 0.f ? 1.0 / b.s : 0.0;
+    b.grown = has_old && b.scale > before;
+    b.ratio = b.grown ? (double)before * b.inv : 1.0;
     return b;
+}
+
+// Queries: a thread rotates pairs 8 o .. 8 o + 7 of `q_heads` heads of a row.
+__device__ __forceinline__ void rotate_queries(const Q8AppendArgs& a, unsigned idx, int tid)
+{
+    const int groups = a.n_q_heads / a.q_heads;
+    const int64_t item = (int64_t)idx * (kThreads / 8) + (tid >> 3);
+    const int o = tid & 7;
+    const int64_t row = item / groups;
+    const int group = (int)(item % groups);
+    if (row >= (int64_t)a.batch * a.m) return;
+    const int n = (int)(row / a.m), j = (int)(row % a.m);
+    const int p = a.length(n) - a.m + j;
+    if (p < 0) return;
+    float c[8], s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const double2 r = angle_of(a.tile_tab[(size_t)(p >> 6) * kQ8Pairs + 8 * o + i], a.lane_tab[lane_entry(p & 63, 8 * o + i)]);
+        c[i] = (float)r.x;
+        s[i] = (float)r.y;
+    }
+    const uint16_t* src = a.q + n * a.q_batch_stride + j * a.q_row_stride + (size_t)group * a.q_heads * kQ8Head + 8 * o;
+    uint16_t* dst = a.q_out + ((size_t)row * a.n_q_heads + (size_t)group * a.q_heads) * kQ8Head + 8 * o;
+#pragma unroll 4
+    for (int h = 0; h < a.q_heads; ++h) {
+        const q8_half8 lo = *reinterpret_cast<const q8_half8*>(src + h * kQ8Head), hi = *reinterpret_cast<const q8_half8*>(src + h * kQ8Head + 64);
+        q8_half8 y, z;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            y[i] = (_Float16)fmaf((float)lo[i], c[i], -(float)hi[i] * s[i]);
+            z[i] = (_Float16)fmaf((float)hi[i], c[i], (float)lo[i] * s[i]);
+        }
+        *reinterpret_cast<q8_half8*>(dst + h * kQ8Head) = y;
+        *reinterpret_cast<q8_half8*>(dst + h * kQ8Head + 64) = z;
+    }
+}
+
+// One token per sequence: a wavefront per sequence and head.  Lane i has channels i and i + 64 of the key and 2 i and 2 i + 1 of the
+// value; older codes are read where their scale grew.
+template <int KIND>
+__global__ __launch_bounds__(kThreads) void append_token_q8_kernel(Q8AppendArgs a)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (blockIdx.x >= a.kv_wgs) return rotate_queries(a, blockIdx.x - a.kv_wgs, tid);
+    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + wave;
+    if (item >= (int64_t)a.batch * a.n_kv_heads) return;
+    const int n = (int)(item / a.n_kv_heads), h = (int)(item % a.n_kv_heads);
+    const int p = a.length(n) - 1;
+    if (p < 0) return;
+    const int tile = p / kTileTokens, u = p % kTileTokens;
+    const size_t at = a.cache.map.tile_index(n, h, tile);
+    const float k_before = u ? a.cache.scales[0][at] : 0.f, v_before = u ? a.cache.scales[1][at] : 0.f;
+    const uint16_t* x_k = a.x[0] + n * a.x_batch_stride + h * kQ8Head;
+    const unsigned v = *reinterpret_cast<const unsigned*>(a.x[1] + n * a.x_batch_stride + h * kQ8Head + 2 * lane);
+    const double x0 = (double)(float)__builtin_bit_cast(_Float16, x_k[lane]), x1 = (double)(float)__builtin_bit_cast(_Float16, x_k[64 + lane]);
+    double y[4] = {x0, x1, (double)(float)__builtin_bit_cast(_Float16, (unsigned short)v), (double)(float)__builtin_bit_cast(_Float16, (unsigned short)(v >> 16))};
+    if (a.tile_tab) {
+        const double2 r = angle_of(a.tile_tab[(size_t)tile * kQ8Pairs + lane], a.lane_tab[lane_entry(u, lane)]);
+        y[0] = fma(x0, r.x, -x1 * r.y);
+        y[1] = fma(x1, r.x, x0 * r.y);
+    }
+    const BlockScale k_scale = block_scale<KIND>(wave_max(fmax(fabs(y[0]), fabs(y[1]))), u > 0, k_before);
+    const BlockScale v_scale = block_scale<KIND>((double)wave_max(largest_half(v & 0x7fff7fffu)), u > 0, v_before);
+    if (lane == 0) {
+        a.cache.scales[0][at] = k_scale.scale;
+        a.cache.scales[1][at] = v_scale.scale;
+    }
+    y[0] = KIND == CQ_Q8_INT8 ? quotient(y[0], k_scale.s, k_scale.inv) : y[0] * k_scale.inv;
+    y[1] = KIND == CQ_Q8_INT8 ? quotient(y[1], k_scale.s, k_scale.inv) : y[1] * k_scale.inv;
+    y[2] = KIND == CQ_Q8_INT8 ? quotient(y[2], v_scale.s, v_scale.inv) : y[2] * v_scale.inv;
+    y[3] = KIND == CQ_Q8_INT8 ? quotient(y[3], v_scale.s, v_scale.inv) : y[3] * v_scale.inv;
+    const unsigned codes = codes4<KIND>(y, 1.0, 1.0);
+    uint8_t* k_dst = a.cache.codes[0] + at * kQ8TileBytes;
+    uint8_t* v_dst = a.cache.codes[1] + at * kQ8TileBytes;
+    k_dst[u * kQ8Head + lane] = (uint8_t)codes;
+    k_dst[u * kQ8Head + 64 + lane] = (uint8_t)(codes >> 8);
+    if (k_scale.grown)
+        for (int i = lane; i < u * (kQ8Head / 16); i += 64) {
+            q8_u4* w = reinterpret_cast<q8_u4*>(k_dst) + i;
+            *w = regrown16<KIND>(*w, k_scale.ratio);
+        }
+    if (!v_scale.grown) {
+        v_dst[2 * lane * kTileTokens + u] = (uint8_t)(codes >> 16);
+        v_dst[(2 * lane + 1) * kTileTokens + u] = (uint8_t)(codes >> 24);
+        return;
+    }
+    // ... of values each 16 bytes hold one channel's: its new one goes into them
+    const int part = lane & 3, from = 16 * part;
+#pragma unroll 2
+    for (int i = 0; i < 8; ++i) {
+        const int channel = 16 * i + (lane >> 2);
+        const unsigned fresh = (unsigned)__shfl((int)codes, channel >> 1) >> (16 + 8 * (channel & 1)) & 0xffu;
+        if (from > u) continue;
+        q8_u4* at_w = reinterpret_cast<q8_u4*>(v_dst + channel * kTileTokens + from);
+        const q8_u4 old = *at_w, now = regrown16<KIND>(old, v_scale.ratio);
+        q8_u4 w;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int before = min(max(u - from - 4 * k, 0), 4);        // bytes of older tokens
+            const unsigned older = (unsigned)((1ULL << (8 * before)) - 1);
+            w[k] = (now[k] & older) | (old[k] & ~older);
+            if (before < 4 && u >= from + 4 * k) w[k] = (w[k] & ~(0xffu << (8 * before))) | fresh << (8 * before);
+        }
+        *at_w = w;
+    }
 }
 
 // A workgroup: one tile of one sequence, `heads` heads in a row, keys or values; behind those, queries.
 template <int KIND>
 __global__ __launch_bounds__(kThreads) void append_q8_kernel(Q8AppendArgs a)
 {
-    __shared__ double lds[kThreads / 64 + 1];               // largest magnitudes of the wavefronts, the scale before
+    __shared__ double lds[2][kThreads / 64];                // largest magnitudes of the wavefronts, of this head and the next
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     unsigned idx = blockIdx.x;
-    if (idx >= 2 * a.kv_wgs) {
-        // ---- queries: a thread rotates pairs 8 o .. 8 o + 7 of `q_heads` heads of a row
-        idx -= 2 * a.kv_wgs;
-        const int groups = a.n_q_heads / a.q_heads;
-        const int64_t item = (int64_t)idx * (kThreads / 8) + (tid >> 3);
-        const int o = tid & 7;
-        const int64_t row = item / groups;
-        const int group = (int)(item % groups);
-        if (row >= (int64_t)a.batch * a.m) return;
-        const int n = (int)(row / a.m), j = (int)(row % a.m);
-        const int p = a.length(n) - a.m + j;
-        if (p < 0) return;
-        float c[8], s[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const double2 r = angle_of(a.tile_tab[(size_t)(p >> 6) * kQ8Pairs + 8 * o + i], a.lane_tab[(p & 63) * kQ8Pairs + 8 * o + i]);
-            c[i] = (float)r.x;
-            s[i] = (float)r.y;
-        }
-        const uint16_t* src = a.q + n * a.q_batch_stride + j * a.q_row_stride + (size_t)group * a.q_heads * kQ8Head + 8 * o;
-        uint16_t* dst = a.q_out + ((size_t)row * a.n_q_heads + (size_t)group * a.q_heads) * kQ8Head + 8 * o;
-#pragma unroll 4
-        for (int h = 0; h < a.q_heads; ++h) {
-            const q8_half8 lo = *reinterpret_cast<const q8_half8*>(src + h * kQ8Head), hi = *reinterpret_cast<const q8_half8*>(src + h * kQ8Head + 64);
-            q8_half8 y, z;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                y[i] = (_Float16)fmaf((float)lo[i], c[i], -(float)hi[i] * s[i]);
-                z[i] = (_Float16)fmaf((float)hi[i], c[i], (float)lo[i] * s[i]);
-            }
-            *reinterpret_cast<q8_half8*>(dst + h * kQ8Head) = y;
-            *reinterpret_cast<q8_half8*>(dst + h * kQ8Head + 64) = z;
-        }
-        return;
-    }
+    if (idx >= 2 * a.kv_wgs) return rotate_queries(a, idx - 2 * a.kv_wgs, tid);
     const int which = idx >= a.kv_wgs;
     idx -= which ? a.kv_wgs : 0;
     const int groups = a.n_kv_heads / a.heads;
@@ -182,10 +274,12 @@ __global__ __launch_bounds__(kThreads) void append_q8_kernel(Q8AppendArgs a)
         double2 ang[16];
         if (a.tile_tab && fresh) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) ang[i] = angle_of(a.tile_tab[(size_t)tile * kQ8Pairs + 16 * o + i], a.lane_tab[u * kQ8Pairs + 16 * o + i]);
+            for (int i = 0; i < 16; ++i) ang[i] = angle_of(a.tile_tab[(size_t)tile * kQ8Pairs + 16 * o + i], a.lane_tab[lane_entry(u, 16 * o + i)]);
         }
-        for (int h = group * a.heads; h < (group + 1) * a.heads; ++h) {
+        for (int i = 0; i < a.heads; ++i) {
+            const int h = group * a.heads + i;
             const size_t at = a.cache.map.tile_index(n, h, tile);
+            const float before = lo > 0 ? a.cache.scales[0][at] : 0.f;
             double x[32], mine = 0.0;
             if (fresh) {
                 const uint16_t* src = x0 + u * a.x_row_stride + h * kQ8Head + 16 * o;
@@ -195,34 +289,32 @@ __global__ __launch_bounds__(kThreads) void append_q8_kernel(Q8AppendArgs a)
                 halves_of(*reinterpret_cast<const q8_u4*>(src + 72), x + 24);
                 if (a.tile_tab) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const double y = fma(x[i], ang[i].x, -x[16 + i] * ang[i].y), z = fma(x[16 + i], ang[i].x, x[i] * ang[i].y);
-                        x[i] = y;
-                        x[16 + i] = z;
+                    for (int k = 0; k < 16; ++k) {
+                        const double y = fma(x[k], ang[k].x, -x[16 + k] * ang[k].y), z = fma(x[16 + k], ang[k].x, x[k] * ang[k].y);
+                        x[k] = y;
+                        x[16 + k] = z;
                     }
                 }
 #pragma unroll
-                for (int i = 0; i < 32; ++i) mine = fmax(mine, fabs(x[i]));
+                for (int k = 0; k < 32; ++k) mine = fmax(mine, fabs(x[k]));
             }
-            const BlockScale b = block_scale<KIND>(mine, lo > 0, a.cache.scales[0] + at, lds, tid);
+            mine = wave_max(mine);
+            double* all = lds[i & 1];
+            if (lane == 0) all[wave] = mine;
+            __syncthreads();
+            const BlockScale b = block_scale<KIND>(fmax(fmax(all[0], all[1]), fmax(all[2], all[3])), lo > 0, before);
+            if (tid == 0) a.cache.scales[0][at] = b.scale;
             uint8_t* dst = a.cache.codes[0] + at * kQ8TileBytes + u * kQ8Head + 16 * o;
             if (fresh) {
-                unsigned w[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    w[i] = 0;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) w[i] |= code_of<KIND>(quotient(x[4 * i + k], b.s, b.inv)) << (8 * k);
-                }
-                *reinterpret_cast<q8_u4*>(dst) = q8_u4{w[0], w[1], w[2], w[3]};
-                *reinterpret_cast<q8_u4*>(dst + 64) = q8_u4{w[4], w[5], w[6], w[7]};
+                for (int k = 0; k < 2; ++k)
+                    *reinterpret_cast<q8_u4*>(dst + 64 * k) = q8_u4{codes4<KIND>(x + 16 * k, b.s, b.inv), codes4<KIND>(x + 16 * k + 4, b.s, b.inv),
+                                                                    codes4<KIND>(x + 16 * k + 8, b.s, b.inv), codes4<KIND>(x + 16 * k + 12, b.s, b.inv)};
             } else if (u < lo && b.grown) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    q8_u4 w = *reinterpret_cast<const q8_u4*>(dst + 64 * k);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = regrown4<KIND>(w[i], b.ratio);
-                    *reinterpret_cast<q8_u4*>(dst + 64 * k) = w;
+                    q8_u4* w = reinterpret_cast<q8_u4*>(dst + 64 * k);
+                    *w = regrown16<KIND>(*w, b.ratio);
                 }
             }
         }
@@ -231,33 +323,71 @@ __global__ __launch_bounds__(kThreads) void append_q8_kernel(Q8AppendArgs a)
     // ---- values: thread (a4, o) holds tokens 4 a4 .. 4 a4 + 3 of channels 8 o .. 8 o + 7, a word of the cache per channel
     const int u = 4 * (lane & 15), o = (lane >> 4) + 4 * wave;
     const bool some_new = u + 4 > lo && u < hi, all_new = u >= lo && u + 4 <= hi;
-    for (int h = group * a.heads; h < (group + 1) * a.heads; ++h) {
+    for (int r = 0; r < a.heads; ++r) {
+        const int h = group * a.heads + r;
         const size_t at = a.cache.map.tile_index(n, h, tile);
-        double mine = 0.0;
-        q8_half8 x[4];
+        const float before = lo > 0 ? a.cache.scales[1][at] : 0.f;
+        unsigned top = 0;
+        q8_u4 x[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if (u + k < lo || u + k >= hi) continue;
-            x[k] = *reinterpret_cast<const q8_half8*>(x0 + (u + k) * a.x_row_stride + h * kQ8Head + 8 * o);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) mine = fmax(mine, fabs((double)(float)x[k][i]));
+            x[k] = q8_u4{0, 0, 0, 0};
+            if (u + k >= lo && u + k < hi) x[k] = *reinterpret_cast<const q8_u4*>(x0 + (u + k) * a.x_row_stride + h * kQ8Head + 8 * o);
         }
-        const BlockScale b = block_scale<KIND>(mine, lo > 0, a.cache.scales[1] + at, lds, tid);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = larger_halves(top, x[k][i]);
+        const float mine = wave_max(largest_half(top));
+        double* all = lds[r & 1];
+        if (lane == 0) all[wave] = mine;
+        __syncthreads();
+        const BlockScale b = block_scale<KIND>(fmax(fmax(all[0], all[1]), fmax(all[2], all[3])), lo > 0, before);
+        if (tid == 0) a.cache.scales[1][at] = b.scale;
         if (!some_new && !(b.grown && u < lo)) continue;
         uint8_t* dst = a.cache.codes[1] + at * kQ8TileBytes + (size_t)(8 * o) * kTileTokens + u;
+        // an fp16 number over a power of two is exact in fp32; of integers' quotients there the code is right unless it lies within
+        // 2^-15 of a border (2^-24 of 127 twice): then all of the thread's are computed as the keys' are
+        unsigned codes[8];
+        const float inv = (float)b.inv;
+        float off = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            unsigned w = 0;
-            if (!all_new) {
-                const unsigned old = *reinterpret_cast<const unsigned*>(dst + i * kTileTokens);
-                const unsigned now = b.grown ? regrown4<KIND>(old, b.ratio) : old;
+            float f[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) w |= (u + k < lo ? now : old) & (0xffu << (8 * k));
+            for (int k = 0; k < 4; ++k) {
+                f[k] = fmaf((float)__builtin_bit_cast(q8_half8, x[k])[i], inv, 0.f);
+                if (KIND == CQ_Q8_INT8) {
+                    const float sum = f[k] + kMagic32;
+                    off = fmaxf(off, fabsf(f[k] - (sum - kMagic32)));
+                    f[k] = sum;
+                }
             }
+            if (KIND == CQ_Q8_INT8)
+                codes[i] = pack_integers(__builtin_bit_cast(unsigned, f[0]), __builtin_bit_cast(unsigned, f[1]), __builtin_bit_cast(unsigned, f[2]), __builtin_bit_cast(unsigned, f[3]));
+            else codes[i] = pack_e4m3(f[0], f[1], f[2], f[3]);
+        }
+        if (KIND == CQ_Q8_INT8 && !(off < 0.5f - 0x1p-15f)) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (u + k >= lo && u + k < hi) w = (w & ~(0xffu << (8 * k))) | code_of<KIND>(quotient((double)(float)x[k][i], b.s, b.inv)) << (8 * k);
-            *reinterpret_cast<unsigned*>(dst + i * kTileTokens) = w;
+            for (int i = 0; i < 8; ++i) {
+                double f[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) f[k] = (double)(float)__builtin_bit_cast(q8_half8, x[k])[i];
+                codes[i] = codes4<KIND>(f, b.s, b.inv);
+            }
+        }
+        if (all_new) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<unsigned*>(dst + i * kTileTokens) = codes[i];
+            continue;
+        }
+        const int olds = min(max(lo - u, 0), 4), news = min(max(hi - u, 0), 4);         // bytes: older tokens', then new ones', then none
+        const unsigned older = (unsigned)((1ULL << (8 * olds)) - 1), fresh = (unsigned)((1ULL << (8 * news)) - 1) & ~older;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            unsigned* w = reinterpret_cast<unsigned*>(dst + i * kTileTokens);
+            const unsigned old = *w, now = b.grown ? regrown4<KIND>(old, b.ratio) : old;
+            *w = (now & older) | (codes[i] & fresh) | (old & ~(older | fresh));
         }
     }
 }
@@ -314,7 +444,7 @@ __global__ __launch_bounds__(kThreads) void dequantize_q8_kernel(Q8DequantArgs a
         if (u + k >= lo && u + k < hi) *reinterpret_cast<q8_half8*>(out + (u + k) * a.out_row_stride + 8 * o) = y[k];
 }
 
-// [tile][pair], then [u][pair]
+// [tile][pair], then entries in the order of lane_entry
 __global__ void q8_rope_table_kernel(double base, int n_tiles, double2* table)
 {
     const int idx = blockIdx.x * blockDim.x + threadIdx.x;
@@ -322,7 +452,7 @@ __global__ void q8_rope_table_kernel(double base, int n_tiles, double2* table)
     const int i = idx % kQ8Pairs, row = idx / kQ8Pairs;
     const double pos = row < n_tiles ? 64.0 * row : (double)(row - n_tiles);
     const double ang = pos * pow(base, -2.0 * (double)i / kQ8Head);
-    table[idx] = make_double2(cos(ang), sin(ang));
+    table[row < n_tiles ? idx : n_tiles * kQ8Pairs + lane_entry(row - n_tiles, i)] = make_double2(cos(ang), sin(ang));
 }
 
 // Tiles of a sequence that its last m tokens can lie in.
@@ -349,11 +479,13 @@ cq_status launch_append_q8(const Q8AppendArgs& args, int kind, hipStream_t strea
 {
     Q8AppendArgs a = args;
     a.slots = tile_slots(a.m, a.t, a.seq_lens != nullptr);
+    // Heads in a row share their angles (64 KB of the table to a tile), as far as 512 workgroups remain: of 256, 512 and 1024, 6 x 500
+    // tokens of 32 heads take 62, 62 and 67 us, 4 x 8192 of 8 heads, 194, 194 and 201 (with the rows read back).
     const int64_t tiles = (int64_t)a.batch * a.slots;
-    // heads in a row share their angles, as far as enough workgroups remain
     a.heads = 1;
-    while (a.heads < 8 && a.n_kv_heads % (2 * a.heads) == 0 && tiles * a.n_kv_heads / (2 * a.heads) >= 1024) a.heads *= 2;
-    const int64_t kv = tiles * (a.n_kv_heads / a.heads);
+    while (a.heads < 8 && a.n_kv_heads % (2 * a.heads) == 0 && tiles * a.n_kv_heads / (2 * a.heads) >= 512) a.heads *= 2;
+    const bool token = a.m == 1;
+    const int64_t kv = token ? ((int64_t)a.batch * a.n_kv_heads + kThreads / 64 - 1) / (kThreads / 64) : tiles * (a.n_kv_heads / a.heads);
     int64_t q_wgs = 0;
     if (a.q) {
         const int64_t rows = (int64_t)a.batch * a.m;
@@ -363,8 +495,11 @@ cq_status launch_append_q8(const Q8AppendArgs& args, int kind, hipStream_t strea
     }
     if (2 * kv + q_wgs > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
     a.kv_wgs = (unsigned)kv;
-    const dim3 grid((unsigned)(2 * kv + q_wgs));
-    if (kind == CQ_Q8_INT8) hipLaunchKernelGGL(append_q8_kernel<CQ_Q8_INT8>, grid, dim3(kThreads), 0, stream, a);
+    const dim3 grid((unsigned)((token ? 1 : 2) * kv + q_wgs));
+    const bool integers = kind == CQ_Q8_INT8;
+    if (token && integers) hipLaunchKernelGGL(append_token_q8_kernel<CQ_Q8_INT8>, grid, dim3(kThreads), 0, stream, a);
+    else if (token) hipLaunchKernelGGL(append_token_q8_kernel<CQ_Q8_E4M3>, grid, dim3(kThreads), 0, stream, a);
+    else if (integers) hipLaunchKernelGGL(append_q8_kernel<CQ_Q8_INT8>, grid, dim3(kThreads), 0, stream, a);
     else hipLaunchKernelGGL(append_q8_kernel<CQ_Q8_E4M3>, grid, dim3(kThreads), 0, stream, a);
     return hipGetLastError() == hipSuccess ? CQ_OK : CQ_ERR_HIP;
 }
