@@ -133,6 +133,25 @@ def test_numbers_at_the_borders_between_codes(kind):
     _same(cache)
 
 
+@pytest.mark.parametrize("step", [1, 64])
+@pytest.mark.parametrize("scale", [3.0, 5.0, 7.0 / 64])
+def test_ties_under_scales_with_inexact_reciprocals(scale, step):
+    """Integers: every code and every half step, exact in fp16, as single tokens and as a tile."""
+    half_steps = np.arange(-253, 254) * scale / 2
+    x = np.zeros((64, D))
+    x.reshape(-1)[2 * D:2 * D + half_steps.size] = half_steps
+    x[0, 127] = 127 * scale                                  # the scale from the first token on
+    assert np.array_equal(x, x.astype(np.float16))
+    x = torch.from_numpy(x).half().cuda().view(1, 64, D)
+    cache = Cache("int8", 1, 1, 64, seed=1)
+    for u in range(0, 64, step):
+        _append(cache, x[:, u:u + step], -x[:, u:u + step], u + step)
+    assert cache.s[0].item() == scale
+    want = np.rint(half_steps / scale).astype(np.int64) + 128
+    assert np.array_equal(cache.k.reshape(-1)[2 * D:2 * D + want.size], want)
+    _same(cache)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_far_positions(kind):
     """Angles of positions near 2^20: the table's last blocks."""
