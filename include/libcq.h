@@ -720,7 +720,7 @@ CQ_API cq_status cq_compact_cache_paged(const void *k_pool, const void *v_pool, 
  * cq_chunk_attention_q8[_paged]    the same for the last m tokens of every sequence, causally.
  *   q, out            device, fp16 [batch][m][n_q_heads][128]
  *   tokens_per_split  0 = the library's choice; otherwise a multiple of 64: the context is cut into pieces of this many tokens
- *                     (of 16384 at most where a KV head has 64 rows, query heads times m, or fewer)
+ *                     (of 16384 at most in calls of few rows, query heads times m, per KV head)
  *   workspace         device, cq_attention_q8_workspace_bytes(...) bytes (decode: m = 1)
  *   Products on the matrix cores: codes (exact in fp16) by fp16 queries, summed in fp32; scores, softmax and sums in fp32;
  *   each weight is rounded to fp16 once where it meets the values' codes (weights of 2^-21 of the largest so far, or more, to

@@ -342,11 +342,19 @@ Q8Plan q8_plan(int batch, int n_kv_heads, int n_q_heads, int m, int t, int token
     const int64_t rows = (int64_t)m * (n_q_heads / n_kv_heads);
     const int n_tiles = (t - 1) / kTileTokens + 1;
     Q8Plan p;
+    // Up to 64 rows of a KV head go by themselves, 16 to a workgroup where the contexts are few tiles (more of them run, and the
+    // codes, read twice, come out of L2), 32 where they are many; more rows share converted tiles through LDS (cq_q8_chunk.hip), where they
+    // are enough work for that.  16 | 32 to a workgroup, us: integers, 32 heads, 20 rows of 4096 16.3 | 20.1, 8 heads, 2 x 64 of 4096 16.9 | 21.4;
+    // 16 x 32 heads, 20 of 4096 117 | 94, 64 x 32, 17 of 300 53 | 47.  32 | 128: 4 x 32 heads, 128 of 2048 31.8 | 41.4, 8 heads, 512 of 4096 26.3 | 27.9,
+    // 8 x 8, 200 of 2000 31 | 35; 8 heads, 512 of 30000 98 | 84, 32 heads, 128 of 16384 65 | 61.
     // Workgroups of eight wavefronts convert a tile half as often as those of four, and reach further in front of their first row and
     // behind their last: where most of the context lies in front of the chunk.  128 -> 256 rows, us: integers, 32 heads, 512 of 16384
     // 166 -> 156, e4m3, 2 x 1024 of 8192 293 -> 271, 32 / 8 heads, 4 x 512 of 16384 568 -> 522; 2 x 4096 of 4096 348 -> 397, with 32 / 8 heads
     // 304 -> 303; 32 / 8 heads, 64 of 8192 27 -> 33.
-    p.row_block = rows <= 16 ? 16 : rows <= 64 ? 32 : rows >= 512 && t - m >= 4096 ? 256 : 128;
+    const int64_t context = (int64_t)batch * n_kv_heads * n_tiles;
+    if (rows <= 64) p.row_block = rows <= 16 || context <= 4096 ? 16 : 32;
+    else if (rows <= 512 && rows * context <= 1 << 19) p.row_block = 32;
+    else p.row_block = rows >= 512 && t - m >= 4096 ? 256 : 128;
     if (tokens_per_split) {
         p.tiles_per_split = p.row_block > 32 ? tokens_per_split / kTileTokens : std::min(tokens_per_split / kTileTokens, kQ8RowTiles);
     } else if (p.row_block > 32) {

@@ -62,7 +62,7 @@ def test_chunk_sizes(kind, hq, hkv, m, t):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("m,hq,hkv", [(6, 4, 4), (70, 8, 2), (150, 2, 1), (300, 4, 4)])
+@pytest.mark.parametrize("m,hq,hkv", [(6, 4, 4), (70, 8, 2), (150, 2, 1), (300, 4, 4), (280, 4, 2)])
 def test_padding_rows_are_zero(kind, m, hq, hkv):
     lens = [0, 1, m - 1, m, m + 1, 300, -5, 9999]
     cache = Cache(kind, hkv, len(lens), 320, seed=m)
@@ -83,7 +83,7 @@ def test_what_lies_behind_a_sequence_does_not_matter(kind, paged):
     """Codes behind the last token, whole tiles and their scales: any bytes (e4m3's no-number too), any scales (no numbers)."""
     lens = [130, 64, 1, 63, 190, 0]
     cache = Cache(kind, 2, 6, 320, seed=5, paged=paged)
-    calls = [(randn((6, 8, D), 1, 2.0), _decode), (randn((6, 3, 8, D), 2, 2.0), _chunk), (randn((6, 90, 8, D), 3, 2.0), _chunk)]
+    calls = [(randn((6, 8, D), 1, 2.0), _decode), (randn((6, 3, 8, D), 2, 2.0), _chunk), (randn((6, 90, 8, D), 3, 2.0), _chunk), (randn((6, 150, 8, D), 4, 2.0), _chunk)]
     want = [f(cache, q, 300, lens) for q, f in calls]
     for n, length in enumerate(lens):
         tile, u = length // TILE, length % TILE
@@ -94,6 +94,26 @@ def test_what_lies_behind_a_sequence_does_not_matter(kind, paged):
     cache.upload()
     for (q, f), w in zip(calls, want):
         assert torch.equal(f(cache, q, 300, lens), w)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("split", [0, 640])
+def test_long_contexts_in_front_of_many_rows(kind, paged, split):
+    """600 rows behind up to 4200 tokens, ragged: all, some and none of the rows have tokens; then what lies behind the sequences changes."""
+    lens = [4800, 650, 4736, 599, 64, 0]
+    cache = Cache(kind, 1, 6, 4864, seed=21, paged=paged)
+    q = randn((6, 600, 1, D), 5, 2.0)
+    out = _chunk(cache, q, 4800, lens, tokens_per_split=split)
+    _check(cache, q, out, 4800, lens)
+    for n, length in enumerate(lens):
+        tile, u = length // TILE, length % TILE
+        cache.k[n, :, tile, u:] = cache.v[n, :, tile, :, u:] = 0x7f
+        cache.k[n, :, tile + 1:] = cache.v[n, :, tile + 1:] = 0xff
+        for x in cache.s:
+            x[n, :, tile + (u > 0):] = np.nan
+    cache.upload()
+    assert torch.equal(_chunk(cache, q, 4800, lens, tokens_per_split=split), out)
 
 
 @pytest.mark.parametrize("kind", KINDS)
@@ -125,7 +145,7 @@ def test_given_splits(kind, split):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("m", [1, 150])
+@pytest.mark.parametrize("m", [1, 150, 300])
 def test_scales_of_every_sign(kind, m):
     cache = Cache(kind, 2, 2, 448, seed=11)
     q = randn((2, m, 4, D), m)
@@ -134,7 +154,7 @@ def test_scales_of_every_sign(kind, m):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("m", [1, 150])
+@pytest.mark.parametrize("m", [1, 150, 300])
 def test_scores_far_beyond_the_24_bits_of_a_float(kind, m):
     """One token's score is larger by 2^20 than all others': its value is the output.  The largest number's own rounding must not
     show."""
@@ -157,7 +177,7 @@ def test_scores_far_beyond_the_24_bits_of_a_float(kind, m):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("m", [1, 130])
+@pytest.mark.parametrize("m", [1, 130, 600])
 def test_many_small_weights_are_not_lost(kind, m):
     """The first token outweighs each of the others by 2^24.5; together they are a few thousandths of the sum, whose values alone are
     not zero in channel 1."""
