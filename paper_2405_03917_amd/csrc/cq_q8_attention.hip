@@ -349,8 +349,8 @@ Q8Plan q8_plan(int batch, int n_kv_heads, int n_q_heads, int m, int t, int token
     // 8 x 8, 200 of 2000 31 | 35; 8 heads, 512 of 30000 98 | 84, 32 heads, 128 of 16384 65 | 61.
     // Workgroups of eight wavefronts convert a tile half as often as those of four, and reach further in front of their first row and
     // behind their last: where most of the context lies in front of the chunk.  128 -> 256 rows, us: integers, 32 heads, 512 of 16384
-    // 166 -> 156, e4m3, 2 x 1024 of 8192 293 -> 271, 32 / 8 heads, 4 x 512 of 16384 568 -> 522; 2 x 4096 of 4096 348 -> 397, with 32 / 8 heads
-    // 304 -> 303; 32 / 8 heads, 64 of 8192 27 -> 33.
+    // 163 -> 155, e4m3, 2 x 1024 of 8192 292 -> 272, 32 / 8 heads, 4 x 512 of 16384 558 -> 523; integers, 32 heads, 2 x 4096 of 4096 309 -> 308, 2000 of
+    // 2000 60 -> 72, ragged 8 x 1024 of 3000 246 -> 256.
     const int64_t context = (int64_t)batch * n_kv_heads * n_tiles;
     if (rows <= 64) p.row_block = rows <= 16 || context <= 4096 ? 16 : 32;
     else if (rows <= 512 && rows * context <= 1 << 19) p.row_block = 32;

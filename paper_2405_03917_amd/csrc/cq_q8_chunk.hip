@@ -8,8 +8,8 @@
 // v_scale / v_largest, an addition to the exponent), and out of their sum again.
 // Bound by the issue of vector and matrix instructions, which keep each other waiting: per 32 rows and tile 64 products of 16
 // clocks and about 200 vector instructions, 32 exponentials among them.  Two wavefronts a SIMD that do nothing but such a mix, on
-// operands from LDS, need 3450 clocks for 2048 of products; here they need 4000.  512 rows' tokens of 16384 (e4m3, 4 x 8 KV heads):
-// 1037 TFLOP/s, integers of 32 heads 830.  (Vector work placed between the products of its own wavefront, wavefronts half a tile apart,
+// operands from LDS, need 3450 clocks for 2048 of products; here they need 4000.  4 x 512 tokens of 16384 (e4m3, 32 / 8 heads): 521 us,
+// 1037 TFLOP/s; 2 x 4096 of 4096 (integers, 32 heads): 308 us, 890, where tiles on the diagonal and the last workgroups count.  (Vector work placed between the products of its own wavefront, wavefronts half a tile apart,
 // 32x32x16 products, keys straight from memory, codes in LDS: 0.95 to 0.7 of that.)
 #include <algorithm>
 
@@ -19,6 +19,10 @@ namespace cq {
 namespace {
 
 constexpr int RB = 2;                                       // blocks of 16 rows of a wavefront
+// Streams (pieces of them) on an XCD whose row blocks are dealt out together, the longest first: more of them end together, fewer share
+// what L2 holds.  1, 2, 4, 8, all, us: integers, 32 heads, 2 x 4096 of 4096 351, 328, 320, 318, 322; 2000 of 2000 75, 75, 60, 60, 61; ragged 8 x 1024 of
+// 3000 269, 260, 255, 256, 264.
+constexpr unsigned kTogether = 4;
 constexpr float kFaintest = -60.f;                          // log2 of a scale relative to the largest, below which it makes no difference
 
 template <int KIND, int WAVES>
@@ -29,10 +33,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs
     extern __shared__ q8_u4 lds[];                          // [2][keys, values][16 operands][64 lanes]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
-    // the row blocks of a piece of a stream run on one XCD, which shares what it reads; the longest first
-    const unsigned eighth = blockIdx.x >> 3;
-    const int block = row_blocks - 1 - (int)(eighth % row_blocks);
-    const unsigned unit = (eighth / row_blocks) * 8 + (blockIdx.x & 7);
+    // the row blocks of a piece of a stream run on one XCD, which shares what it reads; four pieces together, their longest blocks first
+    const unsigned eighth = blockIdx.x >> 3, set = eighth / (kTogether * row_blocks), in_set = eighth % (kTogether * row_blocks);
+    const unsigned here = min(kTogether, (units + 7) / 8 - set * kTogether);
+    const int block = row_blocks - 1 - (int)(in_set / here);
+    const unsigned unit = (set * kTogether + in_set % here) * 8 + (blockIdx.x & 7);
     if (unit >= units) return;
     const int split = unit % a.n_split, stream = unit / a.n_split;
     const int n = stream / a.n_kv_heads, h = stream % a.n_kv_heads;
