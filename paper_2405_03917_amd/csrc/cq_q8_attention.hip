@@ -382,16 +382,18 @@ cq_status launch_attention_q8(const Q8AttentionArgs& args, int kind, const Q8Pla
     a.row_block = plan.row_block;
     const bool chunk = plan.row_block > 32;
     const int64_t blocks = (int64_t)a.batch * a.n_kv_heads * ((a.m * (a.n_q_heads / a.n_kv_heads) - 1) / plan.row_block + 1);
-    // Merging within the kernel saves a launch, and costs each workgroup the way of its partials to memory and back: for small calls
-    // (8 streams of 2000 tokens 10.0 -> 9.0 us, 32 of 4096 12.7 -> 12.3; 256 workgroups in 32 pieces a stream 10.4 -> 12).
-    a.counters = chunk || a.n_split == 1 || a.n_split > 8 || blocks * a.n_split > 256 ? nullptr : merge_counters_for(stream, (int)blocks);
+    // Merging within the kernel saves a launch, and costs the way of the partials to memory and back, by a single workgroup: where they are
+    // few.  us, apart -> within: 1 row of 128 streams, 4 pieces 24.7 -> 22.8, 4 rows of 8, 8 pieces 9.6 -> 9.1, of 192, 3 pieces 45.9 -> 44.7; 16 rows of
+    // 128, 4 pieces 32.3 -> 33.3, 32 of 32, 8 pieces 34.9 -> 39.2; 4 rows of 8 streams, 32 pieces 10.4 -> 12.
+    const int block_rows = std::min(a.m * (a.n_q_heads / a.n_kv_heads), std::min(plan.row_block, 32));
+    a.counters = chunk || a.n_split == 1 || a.n_split > 8 || block_rows * a.n_split > 32 ? nullptr : merge_counters_for(stream, (int)blocks);
     const cq_status st = chunk                 ? launch_chunk_q8(a, kind, plan.row_block, stream)
                          : kind == CQ_Q8_INT8 ? launch_rows<CQ_Q8_INT8>(a, plan.row_block, stream) : launch_rows<CQ_Q8_E4M3>(a, plan.row_block, stream);
     if (st != CQ_OK || a.n_split == 1 || a.counters) return st;
-    const int block_rows = std::min(plan.row_block, 32), row_blocks = (a.m * (a.n_q_heads / a.n_kv_heads) - 1) / block_rows + 1;
+    const int per_merge = std::min(plan.row_block, 32), row_blocks = (a.m * (a.n_q_heads / a.n_kv_heads) - 1) / per_merge + 1;
     const int64_t grid = (int64_t)a.batch * a.n_kv_heads * row_blocks;
     if (grid > 0x7fffffffLL) return CQ_ERR_INVALID_ARG;
-    hipLaunchKernelGGL(merge_q8_kernel, dim3((unsigned)grid), dim3(kThreads), 0, stream, a, row_blocks, block_rows);
+    hipLaunchKernelGGL(merge_q8_kernel, dim3((unsigned)grid), dim3(kThreads), 0, stream, a, row_blocks, per_merge);
     return hipGetLastError() == hipSuccess ? CQ_OK : CQ_ERR_HIP;
 }
 
