@@ -107,6 +107,34 @@ def test_two_captured_steps_replayed():
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("hq,hkv,batch,m,t", [(32, 8, 1, 1, 2000), (32, 32, 2, 1, 2000), (8, 2, 3, 1, 1500), (2, 2, 4, 3, 4000), (12, 4, 2, 2, 900), (64, 2, 2, 1, 1000)])
+def test_pieces_joined_inside_and_apart(hq, hkv, batch, m, t):
+    """A captured call joins its pieces by a launch of its own, an eager one of few partial rows does not: the same bits, whatever
+    order the workgroups ended in, on the stream of the capture and others."""
+    cache = Cache("e4m3", hkv, batch, 4096, seed=t + hq)
+    q = randn((batch, m, hq, D), hq, 2.0)
+    lens = [t - 450 * n for n in range(batch)]
+    assert t > cq.cq_attention_q8_default_split(cache.fmt, batch, hq, m, t)
+    (eager, want), (captured, got) = (cq.prepare_chunk_attention_q8(q, cache.dev, SCALE, cache.fmt, t, **cache.where(lens)) for _ in range(2))
+    eager()
+    _check(cache, q, want, t, lens)
+    first = want.clone()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        captured()
+    for _ in range(4):
+        got.zero_()
+        want.zero_()
+        graph.replay()
+        eager()
+        torch.cuda.synchronize()
+        eager(side)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, first) and torch.equal(want, first)
+
+
 def test_on_another_stream():
     cache = Cache("int8", HKV, 4, 2048, seed=30)
     rope = cq.Q8RopeTable(BASE, 2048)
