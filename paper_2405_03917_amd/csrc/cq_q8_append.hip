@@ -11,7 +11,7 @@
 // fp64 costs what fp32 does here (no packed fp32), but for conversions; of values, which are fp16, fp32 decides where it can.
 // e4m3 scales are powers of two so that a growing scale moves codes without rounding them again (but into
 // subnormals); integers use the whole range instead: a power of two would cost up to a bit of seven.
-// Bound by memory where there is much of it: 4 x 8192 tokens of 8 heads with 32 heads' queries, 738 MB, 153 us; 6 x 500 of 32 heads, 123 MB, 44 us, of
+// Bound by memory where there is much of it: 4 x 8192 tokens of 8 heads with 32 heads' queries, 738 MB, 149 us; 6 x 500 of 32 heads, 123 MB, 42 us, of
 // few workgroups with a reduction each; single tokens by latency: length, page, scale, reduction, division, one after another.
 #include <algorithm>
 
@@ -99,12 +99,6 @@ __device__ __forceinline__ T wave_max(T x)
     return x;
 }
 
-__device__ __forceinline__ void halves_of(q8_u4 w, double* x)
-{
-    const q8_half8 h = __builtin_bit_cast(q8_half8, w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (double)(float)h[i];
-}
 // the larger magnitude of two pairs of fp16 numbers, as bits
 typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ unsigned larger_halves(unsigned a, unsigned b)
@@ -249,7 +243,7 @@ __global__ __launch_bounds__(kThreads) void append_token_q8_kernel(Q8AppendArgs 
 
 // A workgroup: one tile of one sequence, `heads` heads in a row, keys or values; behind those, queries.
 template <int KIND>
-__global__ __launch_bounds__(kThreads) void append_q8_kernel(Q8AppendArgs a)
+__global__ __launch_bounds__(kThreads, 4) void append_q8_kernel(Q8AppendArgs a)
 {
     __shared__ double lds[2][kThreads / 64];                // largest magnitudes of the wavefronts, of this head and the next
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -280,23 +274,38 @@ __global__ __launch_bounds__(kThreads) void append_q8_kernel(Q8AppendArgs a)
             const int h = group * a.heads + i;
             const size_t at = a.cache.map.tile_index(n, h, tile);
             const float before = lo > 0 ? a.cache.scales[0][at] : 0.f;
-            double x[32], mine = 0.0;
-            if (fresh) {
-                const uint16_t* src = x0 + u * a.x_row_stride + h * kQ8Head + 16 * o;
-                halves_of(*reinterpret_cast<const q8_u4*>(src), x);
-                halves_of(*reinterpret_cast<const q8_u4*>(src + 8), x + 8);
-                halves_of(*reinterpret_cast<const q8_u4*>(src + 64), x + 16);
-                halves_of(*reinterpret_cast<const q8_u4*>(src + 72), x + 24);
-                if (a.tile_tab) {
+            // (keys are rotated twice, for their scale and for their codes: held in between, they
+            // would be 64 registers, and 3 wavefronts a SIMD instead of 4: 6 x 500 tokens of 32 heads 62.1 -> 60.4 us, 4 x 8192 of 8 196 -> 192.6,
+            // with the rows read back)
+            q8_u4 raw[4];
+            double mine = 0.0;
+            auto rotated4 = [&](int k, double* y, double* z) {
+                const q8_half8 l = __builtin_bit_cast(q8_half8, raw[k >> 1]), r = __builtin_bit_cast(q8_half8, raw[2 + (k >> 1)]);
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const double y = fma(x[k], ang[k].x, -x[16 + k] * ang[k].y), z = fma(x[16 + k], ang[k].x, x[k] * ang[k].y);
-                        x[k] = y;
-                        x[16 + k] = z;
+                for (int e = 0; e < 4; ++e) {
+                    const double p = (double)(float)l[4 * (k & 1) + e], q = (double)(float)r[4 * (k & 1) + e];
+                    if (a.tile_tab) {
+                        y[e] = fma(p, ang[4 * k + e].x, -q * ang[4 * k + e].y);
+                        z[e] = fma(q, ang[4 * k + e].x, p * ang[4 * k + e].y);
+                    } else {
+                        y[e] = p;
+                        z[e] = q;
                     }
                 }
+            };
+            if (fresh) {
+                const uint16_t* src = x0 + u * a.x_row_stride + h * kQ8Head + 16 * o;
 #pragma unroll
-                for (int k = 0; k < 32; ++k) mine = fmax(mine, fabs(x[k]));
+                for (int k = 0; k < 4; ++k) raw[k] = *reinterpret_cast<const q8_u4*>(src + 64 * (k >> 1) + 8 * (k & 1));
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    double y[4], z[4];
+                    rotated4(k, y, z);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mine = fmax(mine, fmax(fabs(y[e]), fabs(z[e])));
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(raw[k]));
             }
             mine = wave_max(mine);
             double* all = lds[i & 1];
@@ -306,10 +315,16 @@ __global__ __launch_bounds__(kThreads) void append_q8_kernel(Q8AppendArgs a)
             if (tid == 0) a.cache.scales[0][at] = b.scale;
             uint8_t* dst = a.cache.codes[0] + at * kQ8TileBytes + u * kQ8Head + 16 * o;
             if (fresh) {
+                q8_u4 w[2];
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    *reinterpret_cast<q8_u4*>(dst + 64 * k) = q8_u4{codes4<KIND>(x + 16 * k, b.s, b.inv), codes4<KIND>(x + 16 * k + 4, b.s, b.inv),
-                                                                    codes4<KIND>(x + 16 * k + 8, b.s, b.inv), codes4<KIND>(x + 16 * k + 12, b.s, b.inv)};
+                for (int k = 0; k < 4; ++k) {
+                    double y[4], z[4];
+                    rotated4(k, y, z);
+                    w[0][k] = codes4<KIND>(y, b.s, b.inv);
+                    w[1][k] = codes4<KIND>(z, b.s, b.inv);
+                }
+                *reinterpret_cast<q8_u4*>(dst) = w[0];
+                *reinterpret_cast<q8_u4*>(dst + 64) = w[1];
             } else if (u < lo && b.grown) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
