@@ -724,9 +724,9 @@ CQ_API cq_status cq_compact_cache_paged(const void *k_pool, const void *v_pool, 
  *   workspace         device, cq_attention_q8_workspace_bytes(...) bytes (decode: m = 1)
  *   Products on the matrix cores: codes (exact in fp16) by fp16 queries, summed in fp32; scores, softmax and sums in fp32;
  *   each weight is rounded to fp16 once where it meets the values' codes (weights of 2^-21 of the largest so far, or more, to
- *   half a step of fp16; smaller ones to 2^-32 of it.  In calls of many rows a block's weights count in proportion to its value
- *   scale over the largest one so far); the result is rounded to fp16.  Sizes alone choose the kernel and the pieces; no atomics on
- *   results: equal calls give equal bits.  Scores must be finite in fp32.
+ *   half a step of fp16, smaller ones to 2^-32 of it; in calls of many rows 2^-18 and 2^-29); the result is rounded to fp16.
+ *   Sizes alone choose the kernel and the pieces; no atomics on results: equal calls give equal bits.  Scores must be finite in
+ *   fp32.
  * Formats: head_dim 128.  Errors: as cq_decode_attention and cq_encode_kv; CQ_ERR_INVALID_ARG also for an unknown kind, arrays that
  * overlap where one is written, q without a table, and a table that ends before t.
  */

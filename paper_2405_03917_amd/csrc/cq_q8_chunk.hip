@@ -4,12 +4,13 @@
 // and each serve 32 rows.  A tile lies in LDS as the operands of the products, 16 bytes a lane one behind the
 // other, so that neither writing nor reading them meets a bank twice.  Two tiles' room: while one is worked off the next
 // is converted, and the one after that is on its way from memory.
-// Values keep their codes; a block's scale goes into its weights, relative to the largest scale so far (2^(score - reference) by
-// v_scale / v_largest, an addition to the exponent), and out of their sum again.
+// Values keep their codes; a block's scale goes into its weights, relative to the accumulators' unit (2^(score - reference) by
+// v_scale / unit, an addition to the exponent), and out of their sum again.  The unit moves with the scales: weights would lose bits in fp16
+// under one that is far above them.
 // Bound by the issue of vector and matrix instructions, which keep each other waiting: per 32 rows and tile 64 products of 16
 // clocks and about 200 vector instructions, 32 exponentials among them.  Two wavefronts a SIMD that do nothing but such a mix, on
-// operands from LDS, need 3450 clocks for 2048 of products; here they need 4000.  4 x 512 tokens of 16384 (e4m3, 32 / 8 heads): 521 us,
-// 1037 TFLOP/s; 2 x 4096 of 4096 (integers, 32 heads): 308 us, 890, where tiles on the diagonal and the last workgroups count.  (Vector work placed between the products of its own wavefront, wavefronts half a tile apart,
+// operands from LDS, need 3450 clocks for 2048 of products; here they need 4000.  4 x 512 tokens of 16384 (e4m3, 32 / 8 heads): 515 us,
+// 1049 TFLOP/s; 2 x 4096 of 4096 (integers, 32 heads): 308 us, 890, where tiles on the diagonal and the last workgroups count.  (Vector work placed between the products of its own wavefront, wavefronts half a tile apart,
 // 32x32x16 products, keys straight from memory, codes in LDS: 0.95 to 0.7 of that.)
 #include <algorithm>
 
@@ -23,7 +24,8 @@ constexpr int RB = 2;                                       // blocks of 16 rows
 // what L2 holds.  1, 2, 4, 8, all, us: integers, 32 heads, 2 x 4096 of 4096 351, 328, 320, 318, 322; 2000 of 2000 75, 75, 60, 60, 61; ragged 8 x 1024 of
 // 3000 269, 260, 255, 256, 264.
 constexpr unsigned kTogether = 4;
-constexpr float kFaintest = -60.f;                          // log2 of a scale relative to the largest, below which it makes no difference
+constexpr float kFaint = -3.f, kFaintest = -60.f;           // log2 of values' scales relative to the accumulators' unit, and to the largest
+constexpr float kNoScale = -200.f;
 
 template <int KIND, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs a, int row_blocks, unsigned units)
@@ -73,7 +75,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs
 #pragma unroll
         for (int c = 0; c < 8; ++c) o[r][c] = q8_float4{0.f, 0.f, 0.f, 0.f};
     }
-    float largest = 0.f;                                    // of the values' scales so far
+    // log2 of the accumulators' unit: of a scale of the values so far, one that the tile's is between an eighth of and all of (where it is not
+    // below 2^-60 of the largest so far, and makes no difference)
+    float unit_log = kNoScale, largest_log = kNoScale;
 
     // ---- a wavefront brings N of eight parts of keys (part i: tokens b = i / 2, half i & 1 of the channels) and N of values (channel block
     // i), two operands each (as in cq_q8_attention.hip)
@@ -107,14 +111,14 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs
     // its answer (and a scalar request's, for LDS as well).
     int known = tile0;
     size_t places = 0;
-    float k_scales = 0.f, v_scales = 0.f;
+    float k_scales = 0.f, v_logs = 0.f;
     auto learn = [&](int tile) {
         known = tile;
         places = a.cache.map.tile_index(n, h, min(tile + lane, tile1 - 1));
         k_scales = a.cache.scales[0][places];
-        v_scales = a.cache.scales[1][places];
+        v_logs = __builtin_amdgcn_logf(a.cache.scales[1][places]);
         // (waited for here: where they are used, the requests of the next tile would be waited for as well)
-        asm volatile("" : "+v"(k_scales), "+v"(v_scales));
+        asm volatile("" : "+v"(k_scales), "+v"(v_logs));
     };
     auto place = [&](int tile) {
         const int i = tile - known;
@@ -134,7 +138,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs
 #pragma unroll 1
     for (int tile = tile0; tile < tile1; ++tile, buf ^= 1) {
         if (tile - known == 60) learn(tile);
-        const float ks = scale_of(k_scales, tile), vs = scale_of(v_scales, tile);
+        const float ks = scale_of(k_scales, tile), v_log = scale_of(v_logs, tile);
         if (tile + 1 < tile1) {
             stage(tile + 1, buf ^ 1);
             if (tile + 2 < tile1) request(place(tile + 2));
@@ -164,7 +168,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs
                     for (int i = 0; i < 16; ++i) s[r][i >> 2][i & 3] = first + i > pos[r] ? -INFINITY : s[r][i >> 2][i & 3];
             }
             float top[RB];
-            bool over = vs > largest;
+            largest_log = fmaxf(largest_log, v_log);
+            const float next_log = fmaxf(v_log, largest_log + kFaintest);
+            const bool move = v_log > unit_log || (v_log > kNoScale && next_log < unit_log + kFaint);
+            bool over = move;
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
                 float x = s[r][0][0];
@@ -174,8 +181,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs
                 over |= top[r] > ref[r] + kQ8Slack;
             }
             if (__any(over)) {
-                const float v_keep = vs > largest ? largest / vs : 1.f;
-                largest = fmaxf(largest, vs);
+                const float v_keep = move ? __builtin_amdgcn_exp2f(unit_log - next_log) : 1.f;
+                unit_log = move ? next_log : unit_log;
 #pragma unroll
                 for (int r = 0; r < RB; ++r) {
                     top[r] = fmaxf(top[r], __shfl_xor(top[r], 16));
@@ -187,8 +194,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs
                     for (int c = 0; c < 8; ++c) o[r][c] *= keep * v_keep;
                 }
             }
-            const float ratio = largest > 0.f ? vs / largest : 0.f;
-            const float bias = fmaxf(__builtin_amdgcn_logf(ratio), kFaintest), back = __builtin_amdgcn_exp2f(-bias);
+            const float bias = fmaxf(v_log - unit_log, kFaintest), back = __builtin_amdgcn_exp2f(-bias);
             bool wide = false;
 #pragma unroll
             for (int r = 0; r < RB; ++r) wide |= fabsf(ref[r]) > 0x1p20f;
@@ -235,7 +241,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs
         __syncthreads();
     }
 
-    // ---- lane (col, g) holds channels 16 c + 4 g + e of row col, in units of the largest scale
+    // ---- lane (col, g) holds channels 16 c + 4 g + e of row col, in units of 2^unit_log
+    const float v_unit = __builtin_amdgcn_exp2f(unit_log);
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         sum[r] += __shfl_xor(sum[r], 16);
@@ -245,7 +252,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs
         const int j = row / qper;
         const size_t to = ((size_t)n * a.m + j) * a.n_q_heads + h * qper + (row - j * qper);
         if (pieces == 1) {
-            const float by = sum[r] > 0.f ? largest / sum[r] : 0.f;
+            const float by = sum[r] > 0.f ? v_unit / sum[r] : 0.f;
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
                 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
@@ -263,7 +270,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_q8_kernel(Q8AttentionArgs
 #pragma unroll
             for (int c = 0; c < 8; ++c)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) dst[kPartialHeader + 16 * c + 4 * g + e] = o[r][c][e] * largest;
+                for (int e = 0; e < 4; ++e) dst[kPartialHeader + 16 * c + 4 * g + e] = o[r][c][e] * v_unit;
         }
     }
 }

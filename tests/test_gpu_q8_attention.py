@@ -230,6 +230,32 @@ def test_blocks_whose_scales_are_far_apart():
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("m", [1, 200, 600])
+@pytest.mark.parametrize("at", [0, 20])
+def test_small_weights_beside_a_block_of_large_values_without_weight(kind, m, at):
+    """A block whose values are 2^13 times the others' and whose weights are nothing; of the others one token outweighs each by 2^16.3, and
+    the value of the many alone is not zero in channel 1."""
+    t = 4096
+    cache = Cache(kind, 1, 1, t, seed=17, fill=128 if kind == "int8" else 0)
+    one, less = (129, 1) if kind == "int8" else (0x38, 0xf8)    # 1 and -127, 1 and -256
+    for s in cache.s:
+        s[...] = 1.0
+    cache.k[0, 0, 30, 0, 0] = one
+    cache.k[0, 0, at, :, 9] = less
+    cache.v[0, 0, :, 1, :] = one
+    cache.v[0, 0, 30, 1, 0] = 128 if kind == "int8" else 0
+    q = torch.zeros(1, m, 1, D, dtype=torch.float16, device="cuda")
+    q[..., 0] = 16.3 * np.log(2.0)
+    q[..., 9] = 1.0
+    want, tol = cache.attention(q, t, scale=1.0)             # (e^-127 of the weights: no scale of that block would be seen)
+    cache.s[1][0, 0, at] = 2.0 ** 13
+    cache.upload()
+    for split in (0, t):                                     # (cut, few pieces meet the block)
+        off = np.abs(_chunk(cache, q, t, scale=1.0, tokens_per_split=split).cpu().numpy().astype(np.float64) - want)
+        assert (off <= tol).all(), (split, (off / tol).max())
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_equal_calls_give_equal_bits_and_pages_are_no_matter(kind):
     a, b = (Cache(kind, 4, 5, 1024, seed=16, paged=x) for x in (False, True))
     lens = [1000, 1, 500, 64, 999]
