@@ -386,7 +386,7 @@ cq_status launch_attention_q8(const Q8AttentionArgs& args, int kind, const Q8Pla
     // few.  us, apart -> within: 1 row of 128 streams, 4 pieces 24.7 -> 22.8, 4 rows of 8, 8 pieces 9.6 -> 9.1, of 192, 3 pieces 45.9 -> 44.7; 16 rows of
     // 128, 4 pieces 32.3 -> 33.3, 32 of 32, 8 pieces 34.9 -> 39.2; 4 rows of 8 streams, 32 pieces 10.4 -> 12.
     const int block_rows = std::min(a.m * (a.n_q_heads / a.n_kv_heads), std::min(plan.row_block, 32));
-    a.counters = chunk || a.n_split == 1 || a.n_split > 8 || block_rows * a.n_split > 32 ? nullptr : merge_counters_for(stream, (int)blocks);
+    a.counters = chunk || a.n_split == 1 || a.n_split > 8 || block_rows * a.n_split > 32 || blocks > 0x7fffffff ? nullptr : merge_counters_for(stream, (int)blocks);
     const cq_status st = chunk                 ? launch_chunk_q8(a, kind, plan.row_block, stream)
                          : kind == CQ_Q8_INT8 ? launch_rows<CQ_Q8_INT8>(a, plan.row_block, stream) : launch_rows<CQ_Q8_E4M3>(a, plan.row_block, stream);
     if (st != CQ_OK || a.n_split == 1 || a.counters) return st;
