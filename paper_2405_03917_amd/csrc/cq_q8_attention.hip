@@ -8,7 +8,7 @@
 // and block g, rows 4 g + e; rows of key tile b are tokens 16 g + 4 b + e, so a lane's scores of b = 0 .. 3 are tokens 16 g .. 16 g + 15, in
 // order: what the lane feeds into the second product, whose other operand (16 tokens of a channel) is 16 bytes of the cache as they lie.
 // Bound by memory: 16 KB a tile against 512 products' clocks and about 1000 of conversions.  16 x 32 streams of 8192 tokens, 1.07 GB: 178 us,
-// 6.0 TB/s of the 6.4 that a large copy reads at; 24 x 8 of 6007 at most, paged e4m3, 167 MB: 43 us, 3.9; 8 of 2000, 4 MB: 9.0 us, most of it the
+// 6.0 TB/s of the 6.4 that a large read reaches; 24 x 8 of 6007 at most, paged e4m3, 167 MB: 43 us, 3.9; 8 of 2000, 4 MB: 9.0 us, most of it the
 // way of a first request and of the merge.
 #include <algorithm>
 
@@ -152,8 +152,9 @@ __global__ __launch_bounds__(kThreads, 2) void rows_q8_kernel(Q8AttentionArgs a,
         for (int c = 0; c < 8; ++c) o[r][c] = q8_float4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // Codes of a tile: the next one's keys and values each take the place of those they follow.  (Two tiles' registers, all of the next requested
-    // ahead of this one's work, are 2 wavefronts a SIMD instead of 3 for integers: 8 heads x 65536 tokens 28 -> 30 us.)
+    // Codes of a tile: the next one's keys and values each take the place of those they follow.  (Two tiles' registers, all of the next
+    // requested ahead of this one's work, are 2 wavefronts a SIMD instead of 3: 8 streams of 2000 tokens 9.1 -> 8.4 us, of 65536 27.6 -> 28.6, 64 of 32768,
+    // e4m3, 95.4 -> 98.6, 32 of 4096 12.3 -> 13.1.)
     q8_u4 kr[8], vr[8];
     auto request_keys = [&](size_t at) {
         const uint8_t* src = a.cache.codes[0] + at * kQ8TileBytes + (16 * (col >> 2) + (col & 3)) * kQ8Head + 16 * g;
