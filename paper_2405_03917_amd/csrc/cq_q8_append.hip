@@ -58,28 +58,6 @@ __device__ __forceinline__ unsigned codes4(const double* x, double s, double inv
                              low_word(quotient(x[3], s, inv) + kMagic64));
     else return pack_e4m3(to_odd(x[0] * inv), to_odd(x[1] * inv), to_odd(x[2] * inv), to_odd(x[3] * inv));
 }
-// Four codes under a scale that grew by 1 / ratio.
-template <int KIND>
-__device__ __forceinline__ unsigned regrown4(unsigned w, double ratio)
-{
-    double x[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const unsigned byte = (w >> (8 * i)) & 0xffu;
-        x[i] = KIND == CQ_Q8_INT8 ? (double)((int)byte - 128) : (double)__builtin_amdgcn_cvt_f32_fp8((int)byte, 0);
-    }
-    if constexpr (KIND == CQ_Q8_INT8)
-        return pack_integers(low_word(fma(x[0], ratio, kMagic64)), low_word(fma(x[1], ratio, kMagic64)), low_word(fma(x[2], ratio, kMagic64)), low_word(fma(x[3], ratio, kMagic64)));
-    else return codes4<KIND>(x, 1.0, ratio);
-}
-template <int KIND>
-__device__ __forceinline__ q8_u4 regrown16(q8_u4 w, double ratio)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = regrown4<KIND>(w[i], ratio);
-    return w;
-}
-
 template <int KIND>
 __device__ __forceinline__ float need_of(double largest)
 {
@@ -118,10 +96,10 @@ __device__ __forceinline__ double2 angle_of(double2 tile, double2 lane)
 __device__ __forceinline__ int lane_entry(int u, int i) { return ((i & 15) * kTileTokens + u) * (kQ8Pairs / 16) + (i >> 4); }
 
 // A block's scale from the largest new magnitude and the scale before (0 of a block that holds no older tokens); `grown`: the
-// older tokens' codes change by `ratio`.
+// older tokens' codes change.
 struct BlockScale {
-    float scale;
-    double s, inv, ratio;
+    float scale, before;
+    double s, inv;
     bool grown;
 };
 template <int KIND>
@@ -131,9 +109,32 @@ __device__ __forceinline__ BlockScale block_scale(double largest, bool has_old, 
     b.scale = fmaxf(before, need_of<KIND>(largest));
     b.s = b.scale;
     b.inv = b.scale > 0.f ? 1.0 / b.s : 0.0;
+    b.before = before;
     b.grown = has_old && b.scale > before;
-    b.ratio = b.grown ? (double)before * b.inv : 1.0;
     return b;
+}
+// Four older codes of a block whose scale grew.  The numbers they stood for, c s_before, are exact in 64 bits, and go the way of new
+// ones: by a ratio of the scales that is rounded first, ties (every odd code where a scale doubles) would fall to either side.
+template <int KIND>
+__device__ __forceinline__ unsigned regrown4(unsigned w, const BlockScale& b)
+{
+    double x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned byte = (w >> (8 * i)) & 0xffu;
+        x[i] = (double)b.before * (KIND == CQ_Q8_INT8 ? (double)((int)byte - 128) : (double)__builtin_amdgcn_cvt_f32_fp8((int)byte, 0));
+    }
+    return codes4<KIND>(x, b.s, b.inv);
+}
+template <int KIND>
+__device__ __forceinline__ q8_u4 regrown16(q8_u4 w, const BlockScale& b)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[i] = regrown4<KIND>(w[i], b);
+        asm volatile("" : "+v"(w[i]));                      // (a word behind the other: side by side they need registers that the angles hold)
+    }
+    return w;
 }
 
 // Queries: a thread rotates pairs 8 o .. 8 o + 7 of `q_heads` heads of a row.
@@ -213,7 +214,7 @@ __global__ __launch_bounds__(kThreads) void append_token_q8_kernel(Q8AppendArgs 
     if (k_scale.grown)
         for (int i = lane; i < u * (kQ8Head / 16); i += 64) {
             q8_u4* w = reinterpret_cast<q8_u4*>(k_dst) + i;
-            *w = regrown16<KIND>(*w, k_scale.ratio);
+            *w = regrown16<KIND>(*w, k_scale);
         }
     if (!v_scale.grown) {
         v_dst[2 * lane * kTileTokens + u] = (uint8_t)(codes >> 16);
@@ -228,7 +229,7 @@ __global__ __launch_bounds__(kThreads) void append_token_q8_kernel(Q8AppendArgs 
         const unsigned fresh = (unsigned)__shfl((int)codes, channel >> 1) >> (16 + 8 * (channel & 1)) & 0xffu;
         if (from > u) continue;
         q8_u4* at_w = reinterpret_cast<q8_u4*>(v_dst + channel * kTileTokens + from);
-        const q8_u4 old = *at_w, now = regrown16<KIND>(old, v_scale.ratio);
+        const q8_u4 old = *at_w, now = regrown16<KIND>(old, v_scale);
         q8_u4 w;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(kThreads, 4) void append_q8_kernel(Q8AppendArgs a)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     q8_u4* w = reinterpret_cast<q8_u4*>(dst + 64 * k);
-                    *w = regrown16<KIND>(*w, b.ratio);
+                    *w = regrown16<KIND>(*w, b);
                 }
             }
         }
@@ -401,7 +402,7 @@ __global__ __launch_bounds__(kThreads, 4) void append_q8_kernel(Q8AppendArgs a)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             unsigned* w = reinterpret_cast<unsigned*>(dst + i * kTileTokens);
-            const unsigned old = *w, now = b.grown ? regrown4<KIND>(old, b.ratio) : old;
+            const unsigned old = *w, now = b.grown ? regrown4<KIND>(old, b) : old;
             *w = (now & older) | (codes[i] & fresh) | (old & ~(older | fresh));
         }
     }
