@@ -242,8 +242,8 @@ __global__ void decode_merge_kernel(const float* partials, uint16_t* out, int n_
 // what they need is that no two launches that can overlap share a set.  Launches on one stream
 // never overlap, so every stream gets a set of its own (the first kMergeSets streams that ask,
 // per device; a stream keeps its set).  A stream under graph capture gets none: replays of its
-// graph may run on other streams, at the same time as one another.  Whoever gets no set runs
-// the separate merge kernel instead.
+// graph may run on other streams, at the same time as one another.  Nor does hipStreamPerThread: that
+// handle is another stream in every host thread.  Whoever gets no set runs the separate merge kernel instead.
 struct MergeCounters {
     static constexpr int kMaxDevices = 64;
     struct PerDevice {
@@ -257,7 +257,7 @@ struct MergeCounters {
 
     unsigned* for_stream(hipStream_t stream, int rows)
     {
-        if (rows > kMergeRows) return nullptr;
+        if (rows > kMergeRows || stream == hipStreamPerThread) return nullptr;
         hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
         if (hipStreamIsCapturing(stream, &cap) != hipSuccess || cap != hipStreamCaptureStatusNone) {
             (void)hipGetLastError();
@@ -345,11 +345,7 @@ cq_status launch_format(const Args& a, hipStream_t stream)
 
 }  // namespace
 
-unsigned* merge_counters_for(hipStream_t stream, int rows)
-{
-    // (that handle is another stream in every thread)
-    return stream == hipStreamPerThread ? nullptr : g_merge_counters.for_stream(stream, rows);
-}
+unsigned* merge_counters_for(hipStream_t stream, int rows) { return g_merge_counters.for_stream(stream, rows); }
 
 cq_status launch_layer_table_write(const LayerChunk& chunk, int count, LayerPtrs* dst, hipStream_t stream)
 {
