@@ -85,6 +85,24 @@ cq_status check_strided(const void* x, int64_t batch_stride, int64_t row_stride,
     return CQ_OK;
 }
 
+// Whether two arrays of such rows, of the same strides, share an element: rows `apart` elements from one another, or that less
+// whole batch strides and row strides.  All rows of a sequence lie within a batch stride, so two neighbouring multiples of it can do, and of
+// row strides the two next to what is left.
+bool rows_overlap(const void* x, const void* y, int64_t batch_stride, int64_t row_stride, int32_t batch, int32_t m, int64_t width)
+{
+    const uintptr_t p = reinterpret_cast<uintptr_t>(x), q = reinterpret_cast<uintptr_t>(y);
+    const int64_t apart = (int64_t)((p < q ? q - p : p - q) / sizeof(uint16_t));
+    const int64_t first = batch > 1 ? apart / batch_stride : 0;
+    for (int64_t n = first; n <= first + 1 && n < batch; ++n) {
+        const int64_t left = apart - (batch > 1 ? n * batch_stride : 0), within = left < 0 ? -left : left;
+        for (int64_t j = within / row_stride; j <= within / row_stride + 1; ++j) {
+            const int64_t rest = within - j * row_stride;
+            if (j < m && rest < width && -rest < width) return true;
+        }
+    }
+    return false;
+}
+
 void set_rows(Q8Rows* r, const cq_q8_format* fmt, int32_t batch, int32_t m, int32_t t, const int32_t* seq_lens)
 {
     r->batch = batch;
@@ -168,13 +186,7 @@ cq_status dequantize_common(const cq_q8_cache* cache, const cq_q8_format* fmt, i
         if ((st = check_strided(ptr[i], out_batch_stride, out_row_stride, batch, m, width, &out[i])) != CQ_OK) return st;
         if (call.touches(out[i]) || overlap(out[i], Span{seq_lens, seq_lens ? sizeof(int32_t) * batch : 0})) return CQ_ERR_INVALID_ARG;
     }
-    // (two outputs of one buffer, row by row side by side, are apart if one begins behind the other's row)
-    if (k_out && v_out && overlap(out[0], out[1])) {
-        const intptr_t d = static_cast<char*>(v_out) - static_cast<char*>(k_out);
-        const int64_t apart = (d < 0 ? -d : d) / (int64_t)sizeof(uint16_t);
-        const int64_t pitch = m > 1 ? out_row_stride : batch > 1 ? out_batch_stride : 0;
-        if (apart < width || apart + width > pitch) return CQ_ERR_INVALID_ARG;
-    }
+    if (k_out && v_out && rows_overlap(k_out, v_out, out_batch_stride, out_row_stride, batch, m, width)) return CQ_ERR_INVALID_ARG;
     Q8DequantArgs a{};
     set_rows(&a, fmt, batch, m, t, seq_lens);
     a.cache = call.cache;
