@@ -707,7 +707,10 @@ CQ_API cq_status cq_compact_cache_paged(const void *k_pool, const void *v_pool, 
  *   A block that holds older tokens keeps its scale or takes the larger one that the new tokens need; older codes then become
  *   the nearest ones under it.  A block that begins with a new token takes the scale of its new tokens, whatever it held.  What
  *   lies behind t_n is left as it is, and sequences may be cut back (a smaller t_n) at any time.  Codes, nearest with ties to
- *   even, and scales are those of exact arithmetic (the kernel computes in fp64), but for numbers within 2^-45 of a border.
+ *   even, and scales are found in fp64: of keys without a table and of values they are those of exact arithmetic.  Rotated keys are
+ *   off by what their angles are: the frequency theta_i of a pair and its products with positions are rounded to fp64, so a cosine or
+ *   sine at position p is off by 2^-50 + 2^-51 p theta_i at most (2^-39 at 4096, 2^-31 at 2^20) and a number by that times the two of its
+ *   pair; one that near to a border may take the code on its other side.
  *   Equal calls give equal bits; how a prompt is cut into calls changes only codes of blocks that a cut runs through.
  *   Two sequences must not share a page that is written.  Inputs must be finite.
  * cq_q8_rope_table       fills the table of cq_append_q8: fp64 cosines and sines, cq_q8_rope_table_bytes(head_dim, positions) bytes,

@@ -6,8 +6,8 @@
 //   need: integers fp32(largest / 127); e4m3 the smallest power of two >= largest / 448
 //   code = nearest(x / s), ties to even; codes of older tokens, where s grew: nearest(c s_before / s)
 //
-// Which side of a border a number lies on is decided in 64 bits (angles are products of two table entries in 64 bits): codes are
-// those of exact arithmetic but for borders met to 2^-45, whatever the position, and do not depend on how a call is cut.
+// Which side of a border a number lies on is decided in 64 bits, on cosines and sines that are products of two table entries, off by
+// 2^-50 + 2^-51 p th_i at most (th_i and its product with a position are rounded): codes do not depend on how a call is cut.
 // fp64 costs what fp32 does here (no packed fp32), but for conversions; of values, which are fp16, fp32 decides where it can.
 // e4m3 scales are powers of two so that a growing scale moves codes without rounding them again (but into
 // subnormals); integers use the whole range instead: a power of two would cost up to a bit of seven.
