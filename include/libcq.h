@@ -702,7 +702,8 @@ CQ_API cq_status cq_compact_cache_paged(const void *k_pool, const void *v_pool, 
  *   rope_table        device, as written by cq_q8_rope_table, or NULL: keys are stored as they are.  With a table they are rotated
  *                     to their positions first (the rotation of cq_rope_table's calls); rope_positions >= t then, else 0
  *   q                 device, fp16 [batch][m][n_q_heads][128] by element strides q_batch_stride, q_row_stride, or NULL: no queries
- *                     (needs a table).  Rotated to the same positions in the same launch, rounded once
+ *                     (needs a table).  Rotated to the same positions in the same launch: cosines, sines and products in fp32, then
+ *                     rounded to fp16
  *   q_out             device, fp16 [batch][m][n_q_heads][128]; may be q itself where q has no gaps
  *   A block that holds older tokens keeps its scale or takes the larger one that the new tokens need; older codes then become
  *   the nearest ones under it.  A block that begins with a new token takes the scale of its new tokens, whatever it held.  What
@@ -711,13 +712,15 @@ CQ_API cq_status cq_compact_cache_paged(const void *k_pool, const void *v_pool, 
  *   off by what their angles are: the frequency theta_i of a pair and its products with positions are rounded to fp64, so a cosine or
  *   sine at position p is off by 2^-50 + 2^-51 p theta_i at most (2^-39 at 4096, 2^-31 at 2^20) and a number by that times the two of its
  *   pair; one that near to a border may take the code on its other side.
- *   Equal calls give equal bits; how a prompt is cut into calls changes only codes of blocks that a cut runs through.
+ *   Equal calls give equal bits; how a prompt is cut into calls changes only codes of blocks that a cut runs through: there integers
+ *   are rounded again, by up to half a step, each time the scale grows.  Cutting back does not shrink it: until its block begins anew, a
+ *   token that is taken back leaves the scale that it needed, and the coarser codes of the older tokens.
  *   Two sequences must not share a page that is written.  Inputs must be finite.
  * cq_q8_rope_table       fills the table of cq_append_q8: fp64 cosines and sines, cq_q8_rope_table_bytes(head_dim, positions) bytes,
  *                     written asynchronously; arguments as cq_rope_table.
- * cq_dequantize_q8[_paged]   the last m tokens of every sequence as fp16 rows (code times scale, rounded to nearest; a rotated
+ * cq_dequantize_q8[_paged]   the last m tokens of every sequence as fp16 rows (code times scale in fp32, rounded to fp16; a rotated
  *                     key beyond fp16's range becomes infinite).  k_out or v_out may be NULL: not wanted
- *   k_out, v_out      device, fp16 [batch][m][n_kv_heads * 128] by element strides (multiples of 8)
+ *   k_out, v_out      device, fp16 [batch][m][n_kv_heads * 128] by element strides (multiples of 8); may share a buffer where no rows meet
  * cq_decode_attention_q8[_paged]   Eq. 1 for one query token per sequence at position t_n - 1 (t_n = 0: a row of zeros).
  *   q, out            device, fp16 [batch][n_q_heads][128]; query head h reads KV head h / (n_q_heads / n_kv_heads)
  * cq_chunk_attention_q8[_paged]    the same for the last m tokens of every sequence, causally.
@@ -727,7 +730,8 @@ CQ_API cq_status cq_compact_cache_paged(const void *k_pool, const void *v_pool, 
  *   workspace         device, cq_attention_q8_workspace_bytes(...) bytes (decode: m = 1)
  *   Products on the matrix cores: codes (exact in fp16) by fp16 queries, summed in fp32; scores, softmax and sums in fp32;
  *   each weight is rounded to fp16 once where it meets the values' codes (weights of 2^-21 of the largest so far, or more, to
- *   half a step of fp16, smaller ones to 2^-32 of it; in calls of many rows 2^-18 and 2^-29); the result is rounded to fp16.
+ *   half a step of fp16, smaller ones to 2^-32 of it; in calls of many rows, where a block's value scale enters its weights through its
+ *   logarithm in fp32, 2^-18 and 2^-29); the result is rounded to fp16.
  *   Sizes alone choose the kernel and the pieces; no atomics on results: equal calls give equal bits.  Scores must be finite in
  *   fp32.
  * Formats: head_dim 128.  Errors: as cq_decode_attention and cq_encode_kv; CQ_ERR_INVALID_ARG also for an unknown kind, arrays that

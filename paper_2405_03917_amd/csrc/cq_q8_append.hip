@@ -137,7 +137,8 @@ __device__ __forceinline__ q8_u4 regrown16(q8_u4 w, const BlockScale& b)
     return w;
 }
 
-// Queries: a thread rotates pairs 8 o .. 8 o + 7 of `q_heads` heads of a row.
+// Queries: a thread rotates pairs 8 o .. 8 o + 7 of `q_heads` heads of a row, in fp32 (2^-24 of a product is nothing beside the 2^-11 of
+// the fp16 they are rounded to).
 __device__ __forceinline__ void rotate_queries(const Q8AppendArgs& a, unsigned idx, int tid)
 {
     const int groups = a.n_q_heads / a.q_heads;

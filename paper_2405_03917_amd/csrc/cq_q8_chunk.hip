@@ -9,8 +9,9 @@
 // under one that is far above them.
 // Bound by the issue of vector and matrix instructions, which keep each other waiting: per 32 rows and tile 64 products of 16
 // clocks and about 200 vector instructions, 32 exponentials among them.  Two wavefronts a SIMD that do nothing but such a mix, on
-// operands from LDS, need 3450 clocks for 2048 of products; here they need 4000.  4 x 512 tokens of 16384 (e4m3, 32 / 8 heads): 515 us,
-// 1049 TFLOP/s; 2 x 4096 of 4096 (integers, 32 heads): 308 us, 890, where tiles on the diagonal and the last workgroups count.  (Vector work placed between the products of its own wavefront, wavefronts half a tile apart,
+// operands from LDS, need 3450 clocks for 2048 of products; here they need 4000.  4 x 512 tokens of 16384 (e4m3, 32 / 8 heads): 515 to 521 us
+// by the card, 1049 to 1038 TFLOP/s; 2 x 4096 of 4096 (integers, 32 heads): 303 to 314, 908 to 877, where tiles on the diagonal and the last
+// workgroups count.  (Vector work placed between the products of its own wavefront, wavefronts half a tile apart,
 // 32x32x16 products, keys straight from memory, codes in LDS: 0.95 to 0.7 of that.)
 #include <algorithm>
 
