@@ -96,10 +96,10 @@ __device__ __forceinline__ double2 angle_of(double2 tile, double2 lane)
 __device__ __forceinline__ int lane_entry(int u, int i) { return ((i & 15) * kTileTokens + u) * (kQ8Pairs / 16) + (i >> 4); }
 
 // A block's scale from the largest new magnitude and the scale before (0 of a block that holds no older tokens); `grown`: the
-// older tokens' codes change.
+// older tokens' codes change by `ratio`.
 struct BlockScale {
-    float scale, before;
-    double s, inv;
+    float scale;
+    double s, inv, ratio;
     bool grown;
 };
 template <int KIND>
@@ -109,12 +109,15 @@ __device__ __forceinline__ BlockScale block_scale(double largest, bool has_old, 
     b.scale = fmaxf(before, need_of<KIND>(largest));
     b.s = b.scale;
     b.inv = b.scale > 0.f ? 1.0 / b.s : 0.0;
-    b.before = before;
     b.grown = has_old && b.scale > before;
+    b.ratio = b.grown ? (double)before * b.inv : 1.0;
     return b;
 }
-// Four older codes of a block whose scale grew.  The numbers they stood for, c s_before, are exact in 64 bits, and go the way of new
-// ones: by a ratio of the scales that is rounded first, ties (every odd code where a scale doubles) would fall to either side.
+// Four older codes of a block whose scale grew by 1 / ratio.  Of integers the ratio is rounded (twice: 2^-52 of it), and ties, every odd code
+// where a scale doubles, must not fall to either side for that.  So c ratio is rounded to a multiple of 2^-36 first (the last place
+// of 1.5 x 2^16 and a little): from within 2^-45 a tie comes back to itself, and what is no tie stays on its side, 2^-32 away or more.
+// (c b / s - (k + 1/2) is (2 c b - (2 k + 1) s) / 2 s, of 24-bit b and s with s < 2^8 b where half a step is reached at all.)
+constexpr double kSnap64 = 98304.0;
 template <int KIND>
 __device__ __forceinline__ unsigned regrown4(unsigned w, const BlockScale& b)
 {
@@ -122,18 +125,17 @@ __device__ __forceinline__ unsigned regrown4(unsigned w, const BlockScale& b)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const unsigned byte = (w >> (8 * i)) & 0xffu;
-        x[i] = (double)b.before * (KIND == CQ_Q8_INT8 ? (double)((int)byte - 128) : (double)__builtin_amdgcn_cvt_f32_fp8((int)byte, 0));
+        x[i] = KIND == CQ_Q8_INT8 ? (double)((int)byte - 128) : (double)__builtin_amdgcn_cvt_f32_fp8((int)byte, 0);
+        if (KIND == CQ_Q8_INT8) x[i] = fma(x[i], b.ratio, kSnap64) + (kMagic64 - kSnap64);
     }
-    return codes4<KIND>(x, b.s, b.inv);
+    if constexpr (KIND == CQ_Q8_INT8) return pack_integers(low_word(x[0]), low_word(x[1]), low_word(x[2]), low_word(x[3]));
+    else return codes4<KIND>(x, 1.0, b.ratio);
 }
 template <int KIND>
 __device__ __forceinline__ q8_u4 regrown16(q8_u4 w, const BlockScale& b)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        w[i] = regrown4<KIND>(w[i], b);
-        asm volatile("" : "+v"(w[i]));                      // (a word behind the other: side by side they need registers that the angles hold)
-    }
+    for (int i = 0; i < 4; ++i) w[i] = regrown4<KIND>(w[i], b);
     return w;
 }
 
